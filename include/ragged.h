@@ -449,6 +449,43 @@ rag_status encoder_layer_noalloc(const rag_plan* plan, const void* x, void* y, i
                                  int32_t heads, int32_t head_dim, int32_t d_ff, float ln_eps, int32_t act,
                                  int32_t flags, const rag_layer_weights* w, int32_t dtype, void* stream);
 
+/*
+ * The operators of a decoder layer with 8-bit projections.  They read and write
+ * packed activations like the operators above (dtype RAG_BF16 or RAG_F32) and
+ * hold sums, statistics and softmax states in fp32 (products of 8-bit integers in
+ * int32, exactly; angles in fp64).
+ *
+ * 8-bit rows: row t of an [rows, d] matrix is int8 q and one fp32 scale, its values
+ * q[t][c] * scale[t], with scale[t] = max_c |y[t][c]| / 127 and q = y / scale rounded
+ * to nearest even (never -128).  A row whose scale would be subnormal (all zeros
+ * among them) gets scale 0 and q = 0; a row that holds an infinity or a NaN gets
+ * scale NaN and q = 0, so that whatever is computed from it is NaN.
+ */
+
+/*
+ * Root-mean-square norm over the d features of each of T token rows, with the
+ * residual's addition before it:
+ *   h = x + residual;   y = gamma * h / sqrt(mean(h^2) + eps)
+ * residual [T, d] (ldr) or NULL (h = x).  `sum` [T, d] (lds) or NULL receives h
+ * rounded to dtype; the norm is taken of h before that rounding.  The norm's
+ * outputs, at least one of them non-NULL: `y` [T, d] (ldy) in dtype, and `q` int8
+ * [T, d] (ldq) with `q_scale` fp32 [T], the 8-bit rows of y before its rounding.
+ * d is a multiple of E = 8 (bf16) or 4 (fp32), d <= 16384, eps positive and finite; q is
+ * E-byte aligned with ldq % E == 0.  sum and y may each equal x or residual (same ld),
+ * and overlap nothing otherwise.  With T == 0 the data pointers may be NULL.
+ */
+#define RAG_NORM_MAX_DIM 16384
+rag_status packed_rmsnorm(const void* x, int32_t ldx, const void* residual, int32_t ldr, const void* gamma,
+                          float eps, void* sum, int32_t lds, void* y, int32_t ldy, int8_t* q, int32_t ldq,
+                          float* q_scale, int32_t T, int32_t d, int32_t dtype, void* stream);
+
+/*
+ * 8-bit rows of x [T, d]: tokens for packed_linear_i8, or a weight matrix (its
+ * rows are the output channels).  Shapes and alignment as in packed_rmsnorm.
+ */
+rag_status packed_quantize_i8(const void* x, int32_t ldx, int8_t* q, int32_t ldq, float* scale, int32_t T,
+                              int32_t d, int32_t dtype, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -87,6 +87,8 @@ _c_attn_v_causal = _sig("ragged_attn_v_causal", list(_c_attn_v.argtypes))
 _c_attention_causal = _sig("ragged_attention_causal", list(_c_attention.argtypes))
 _c_linear = _sig("packed_linear", [_p, _i32, _p, _p, _p, _i32, _i32, _p, _i32, _i32, _i32, _i32, _i32, _p])
 _c_layernorm = _sig("packed_layernorm", [_p, _i32, _p, _p, _f32, _p, _i32, _i32, _i32, _i32, _p])
+_c_rmsnorm = _sig("packed_rmsnorm", [_p, _i32, _p, _i32, _p, _f32, _p, _i32, _p, _i32, _p, _i32, _p, _i32, _i32, _i32, _p])
+_c_quantize_i8 = _sig("packed_quantize_i8", [_p, _i32, _p, _i32, _p, _i32, _i32, _i32, _p])
 _c_vgemm_capacity = _sig("vgemm_plan_capacity", [_i32, _i32, _i32, ctypes.POINTER(_i64)])
 _c_vgemm_tile_count = _sig("vgemm_tile_count", [_i32, _p, ctypes.POINTER(_i64)])
 _c_vgemm_offsets = _sig("vgemm_offsets", [ctypes.POINTER(RagVgemmPlan), _p])
@@ -254,6 +256,43 @@ def packed_layernorm(x, gamma, beta, y, eps=1e-5, stream=None):
     T, d = x.shape
     _check("packed_layernorm", _c_layernorm(_ptr(x), _ld(x), _ptr(gamma), _ptr(beta), eps, _ptr(y), _ld(y), T, d,
                                             _dtype_code(x), _stream(stream)))
+
+
+def _like(name, t, shape, dtype):
+    """`t` is None or a tensor of this shape and type."""
+    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
+        raise ValueError(f"{name} must be {list(shape)} of {dtype}, not {list(t.shape)} of {t.dtype}")
+
+
+def _vector(name, t, n, dtype):
+    """`t` is None or a contiguous vector of n elements."""
+    _like(name, t, (n,), dtype)
+    if t is not None and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def packed_rmsnorm(x, gamma, y=None, eps=1e-6, residual=None, x_out=None, q=None, q_scale=None, stream=None):
+    """h = x + residual, and its RMS norm times gamma: into `y`, into the 8-bit rows `q` (int8)
+    and `q_scale` (float32 [T]), or both; `x_out` receives h.  `y` and `x_out` may be x or residual."""
+    T, d = x.shape
+    for name, t in (("y", y), ("residual", residual), ("x_out", x_out)):
+        _like(name, t, x.shape, x.dtype)
+    _vector("gamma", gamma, d, x.dtype)
+    _like("q", q, x.shape, torch.int8)
+    _vector("q_scale", q_scale, T, torch.float32)
+    ld = [0 if t is None else _ld(t) for t in (residual, x_out, y, q)]
+    _check("packed_rmsnorm", _c_rmsnorm(_ptr(x), _ld(x), _ptr(residual), ld[0], _ptr(gamma), eps, _ptr(x_out), ld[1],
+                                        _ptr(y), ld[2], _ptr(q), ld[3], _ptr(q_scale), T, d, _dtype_code(x),
+                                        _stream(stream)))
+
+
+def packed_quantize_i8(x, q, scale, stream=None):
+    """8-bit rows of x [T, d] (tokens, or a weight matrix): q int8 [T, d], scale float32 [T]."""
+    T, d = x.shape
+    _like("q", q, x.shape, torch.int8)
+    _vector("scale", scale, T, torch.float32)
+    _check("packed_quantize_i8", _c_quantize_i8(_ptr(x), _ld(x), _ptr(q), _ld(q), _ptr(scale), T, d, _dtype_code(x),
+                                                _stream(stream)))
 
 
 def encoder_layer_workspace(total_tokens, max_len, d_model, heads, d_ff, dtype=RAG_BF16, flags=0):

@@ -607,4 +607,103 @@ rag_status ragged_trmm(const void* l, int32_t ldl, const void* b, int32_t ldb, v
     return finish(rag::launch_trmm(dtype, l, ldl, b, ldb, c, ldc, n, m, s), s, nullptr, fn);
 }
 
+namespace {
+
+// Rows read and written in 16-byte chunks in either type.
+rag_status check_rows(const void* ptr, int64_t ld, int64_t width, int32_t dtype, const char* name, const char* fn) {
+    const rag_status st = check_operand(ptr, ld, width, dtype, 16, name, fn);
+    if (st) return st;
+    if (!aligned(ptr, 16) || ld * (int64_t)elem_size(dtype) % 16 != 0)
+        return fail(RAG_ERR_SHAPE, "%s: %s needs 16-byte aligned rows", fn, name);
+    return RAG_OK;
+}
+
+size_t span8(int64_t rows, int64_t ld, int64_t width) { return rows > 0 ? (size_t)((rows - 1) * ld + width) : 0; }
+
+// An output in 8-bit rows of per-element chunks of E values.
+rag_status check_q(const int8_t* q, int64_t ldq, const float* scale, int64_t d, int E, const char* fn) {
+    if (!q || !scale) return fail(RAG_ERR_ARG, "%s: q and its scale go together", fn);
+    if (ldq < d) return fail(RAG_ERR_SHAPE, "%s: leading dimension of q (%lld) < width %lld", fn, (long long)ldq, (long long)d);
+    if (!aligned(q, E) || ldq % E != 0)
+        return fail(RAG_ERR_SHAPE, "%s: q must be %d-byte aligned with a leading dimension that is a multiple of %d", fn, E, E);
+    if (!aligned(scale, 4)) return fail(RAG_ERR_SHAPE, "%s: scale misaligned", fn);
+    return RAG_OK;
+}
+
+rag_status check_norm_sizes(int32_t T, int32_t d, int32_t dtype, const char* fn) {
+    const rag_status st = check_dtype(dtype, fn);
+    if (st) return st;
+    if (T < 0 || d < 1) return fail(RAG_ERR_ARG, "%s: T %d, d %d out of range", fn, T, d);
+    const int E = dtype == RAG_BF16 ? 8 : 4;
+    if (d % E != 0 || d > RAG_NORM_MAX_DIM)
+        return fail(RAG_ERR_SHAPE, "%s: d %d must be a multiple of %d and <= %d", fn, d, E, RAG_NORM_MAX_DIM);
+    return RAG_OK;
+}
+
+struct Span {
+    const void* p;
+    size_t n;
+    int64_t ld;
+};
+
+// Outputs against inputs they may equal exactly (same address and row stride) and against
+// everything else.
+bool clash(const Span& out, const Span& in) {
+    if (!out.p || !in.p || !ranges_overlap(out.p, out.n, in.p, in.n)) return false;
+    return !(out.p == in.p && out.ld == in.ld);
+}
+
+}  // namespace
+
+rag_status packed_rmsnorm(const void* x, int32_t ldx, const void* residual, int32_t ldr, const void* gamma, float eps,
+                          void* sum, int32_t lds, void* y, int32_t ldy, int8_t* q, int32_t ldq, float* q_scale,
+                          int32_t T, int32_t d, int32_t dtype, void* stream) {
+    const char* fn = "packed_rmsnorm";
+    rag_status st;
+    if ((st = check_norm_sizes(T, d, dtype, fn))) return st;
+    if (!(eps > 0.f) || !std::isfinite(eps)) return fail(RAG_ERR_ARG, "%s: eps must be positive and finite", fn);
+    if (T == 0) return RAG_OK;  // nothing is read or written
+    if ((st = check_rows(x, ldx, d, dtype, "x", fn))) return st;
+    if (residual && (st = check_rows(residual, ldr, d, dtype, "residual", fn))) return st;
+    if (!gamma || !aligned(gamma, 16)) return fail(RAG_ERR_ARG, "%s: gamma NULL or misaligned", fn);
+    if (!y && !q) return fail(RAG_ERR_ARG, "%s: neither y nor q is given", fn);
+    if (sum && (st = check_rows(sum, lds, d, dtype, "sum", fn))) return st;
+    if (y && (st = check_rows(y, ldy, d, dtype, "y", fn))) return st;
+    if ((q || q_scale) && (st = check_q(q, ldq, q_scale, d, dtype == RAG_BF16 ? 8 : 4, fn))) return st;
+    const Span sx{x, span_bytes(T, ldx, d, dtype), ldx}, sr{residual, span_bytes(T, ldr, d, dtype), ldr};
+    const Span sg{gamma, d * elem_size(dtype), 0};
+    const Span ss{sum, span_bytes(T, lds, d, dtype), lds}, sy{y, span_bytes(T, ldy, d, dtype), ldy};
+    const Span sq{q, q ? span8(T, ldq, d) : 0, -1}, sc{q_scale, (size_t)T * 4, -2};
+    if (clash(ss, sx) || clash(ss, sr) || clash(sy, sx) || clash(sy, sr))
+        return fail(RAG_ERR_ARG, "%s: sum or y partially overlaps x or residual", fn);
+    const Span outs[4] = {ss, sy, sq, sc};
+    for (int i = 0; i < 4; ++i) {
+        if (outs[i].p && ranges_overlap(outs[i].p, outs[i].n, sg.p, sg.n)) return fail(RAG_ERR_ARG, "%s: an output overlaps gamma", fn);
+        for (int j = i + 1; j < 4; ++j)
+            if (outs[i].p && outs[j].p && ranges_overlap(outs[i].p, outs[i].n, outs[j].p, outs[j].n))
+                return fail(RAG_ERR_ARG, "%s: two outputs overlap", fn);
+    }
+    if (clash(sq, sx) || clash(sq, sr) || clash(sc, sx) || clash(sc, sr))
+        return fail(RAG_ERR_ARG, "%s: q or its scale overlaps x or residual", fn);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return finish(rag::launch_rmsnorm(dtype, x, ldx, residual, ldr, gamma, eps, sum, lds, y, ldy, q, ldq, q_scale, T, d, s),
+                  s, nullptr, fn);
+}
+
+rag_status packed_quantize_i8(const void* x, int32_t ldx, int8_t* q, int32_t ldq, float* scale, int32_t T, int32_t d,
+                              int32_t dtype, void* stream) {
+    const char* fn = "packed_quantize_i8";
+    rag_status st;
+    if ((st = check_norm_sizes(T, d, dtype, fn))) return st;
+    if (T == 0) return RAG_OK;
+    if ((st = check_rows(x, ldx, d, dtype, "x", fn)) || (st = check_q(q, ldq, scale, d, dtype == RAG_BF16 ? 8 : 4, fn)))
+        return st;
+    const Span sx{x, span_bytes(T, ldx, d, dtype), ldx};
+    const Span sq{q, span8(T, ldq, d), -1}, sc{scale, (size_t)T * 4, -2};
+    if (clash(sq, sx) || clash(sc, sx) || ranges_overlap(sq.p, sq.n, sc.p, sc.n))
+        return fail(RAG_ERR_ARG, "%s: x, q and scale overlap", fn);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return finish(rag::launch_quantize_i8(dtype, x, ldx, q, ldq, scale, T, d, s), s, nullptr, fn);
+}
+
 }  // extern "C"

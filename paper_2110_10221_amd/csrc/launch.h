@@ -78,4 +78,11 @@ hipError_t launch_trmm(int dtype, const void* l, int ldl, const void* b, int ldb
 hipError_t launch_layernorm(int dtype, const void* x, int ldx, const void* gamma, const void* beta,
                             float eps, void* y, int ldy, int T, int d, hipStream_t s);
 
+// RMS norm with the residual's addition (residual, sum, y and q may be NULL), and 8-bit rows.
+hipError_t launch_rmsnorm(int dtype, const void* x, int ldx, const void* residual, int ldr, const void* gamma, float eps,
+                          void* sum, int lds, void* y, int ldy, int8_t* q, int ldq, float* q_scale, int T, int d,
+                          hipStream_t s);
+hipError_t launch_quantize_i8(int dtype, const void* x, int ldx, int8_t* q, int ldq, float* scale, int T, int d,
+                              hipStream_t s);
+
 }  // namespace rag

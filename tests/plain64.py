@@ -1,0 +1,47 @@
+"""Plain 64-bit forms of the 8-bit decoder operators (torch on the CPU), written from their
+definitions; the tests compare the kernels with them.
+
+Half steps, as multiples of a value: bf16 2^-8, fp32 2^-24."""
+from __future__ import annotations
+
+import math
+
+import torch
+
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+
+
+def normal(seed, *shape, dtype="bf16", std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g, dtype=torch.float64) * std).to(TYPES[dtype])
+
+
+def strided(t, pad, device="cuda"):
+    """The same rows on the device with `pad` elements of NaN (of -99 in int8) behind each."""
+    fill = -99 if t.dtype == torch.int8 else float("nan")
+    whole = torch.full((t.shape[0], t.shape[1] + pad), fill, dtype=t.dtype, device=device)
+    whole[:, :t.shape[1]] = t.to(device)
+    return whole[:, :t.shape[1]]
+
+
+def rmsnorm(x, gamma, eps, residual=None):
+    """(h, y) in float64."""
+    h = x.double() + (0.0 if residual is None else residual.double())
+    return h, gamma.double() * h / torch.sqrt((h * h).mean(1, keepdim=True) + eps)
+
+
+def eight(y):
+    """(q, scale) of float64 rows, and how far y / scale is from a border between two steps."""
+    scale = y.abs().amax(1) / 127.0
+    scale = torch.where(scale < 2.0 ** -126, 0.0, scale)
+    z = torch.where(scale[:, None] > 0, y / scale[:, None], 0.0)
+    return torch.round(z), scale, (z - torch.floor(z) - 0.5).abs()
+
+
+def gelu(y, act):
+    if act == 1:
+        return 0.5 * y * (1.0 + torch.erf(y / math.sqrt(2.0)))
+    if act == 2:
+        return 0.5 * y * (1.0 + torch.tanh(math.sqrt(2.0 / math.pi) * (y + 0.044715 * y ** 3)))
+    return y
