@@ -486,6 +486,50 @@ rag_status packed_rmsnorm(const void* x, int32_t ldx, const void* residual, int3
 rag_status packed_quantize_i8(const void* x, int32_t ldx, int8_t* q, int32_t ldq, float* scale, int32_t T,
                               int32_t d, int32_t dtype, void* stream);
 
+/*
+ * Rotary positions.  Pair i of a head turns by the angle p * inv_freq[i] at position p:
+ *   (a, b) -> amplitude * (a cos - b sin, a sin + b cos)
+ * over the first rot_dim channels of each head; the others pass unchanged.
+ */
+enum { RAG_ROTARY_HALF = 0,        /* pair i is channels i and i + rot_dim / 2        */
+       RAG_ROTARY_INTERLEAVED = 1, /* pair i is channels 2i and 2i + 1                */
+       RAG_ROTARY_INVERSE = 2 };   /* added to a layout: turns by minus the angle (the
+                                      transpose: what a gradient takes back)          */
+/* Frequencies for contexts `factor` times longer than trained on. */
+enum { RAG_ROTARY_PLAIN = 0,  /* base^(-2i / rot_dim)                                          */
+       RAG_ROTARY_LINEAR = 1, /* those over factor (positions interpolated)                    */
+       RAG_ROTARY_NTK = 2,    /* base * factor^(rot_dim / (rot_dim - 2)) as the base           */
+       RAG_ROTARY_YARN = 3 }; /* Peng et al., YaRN: pairs that turn more than beta_fast times over
+                                 orig_len positions keep their frequency, below beta_slow it is
+                                 divided by factor, a ramp between; amplitude 0.1 ln(factor) + 1 */
+
+/*
+ * (host only)  inv_freq[rot_dim / 2] (host) and amplitude (host) of one of the rules
+ * above.  rot_dim even in [2, RAG_ROTARY_MAX_DIM], base > 1; factor >= 1 and finite (ignored by
+ * RAG_ROTARY_PLAIN); RAG_ROTARY_YARN also reads orig_len >= 1 and beta_fast >=
+ * beta_slow > 0, the others ignore them.  Launches nothing.
+ */
+#define RAG_ROTARY_MAX_DIM 512
+rag_status rotary_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, int32_t orig_len,
+                              double beta_fast, double beta_slow, double* inv_freq /* (host) out */,
+                              double* amplitude /* (host) out */);
+
+/*
+ * Rotary positions of `heads` heads of head_dim channels (any number of heads: the
+ * query and key columns of a QKV row are turned in one call), row t of x [T, heads *
+ * head_dim] (ldx) into y (ldy), T = plan->total_tokens.  Token t of sequence b is at
+ * position t - tok_off[b] + pos_start[b] (pos_start int32 [B] or NULL for 0).
+ * inv_freq is fp64 [rot_dim / 2] in device memory.  rot_dim even, 2 <= rot_dim <=
+ * head_dim <= RAG_ROTARY_MAX_DIM.  Angles are reduced in fp64, so positions up to 2^31 keep fp32
+ * accuracy.  y may equal x (same ld) and overlaps nothing otherwise.  x and y need
+ * only their element's alignment; 16-byte aligned rows, head_dim and (for
+ * RAG_ROTARY_HALF half of) rot_dim in multiples of 16 bytes run several times faster.
+ * After a data error of the plan nothing is written.
+ */
+rag_status packed_rotary(const rag_plan* plan, const void* x, int32_t ldx, void* y, int32_t ldy, int32_t heads,
+                         int32_t head_dim, int32_t rot_dim, int32_t layout, const double* inv_freq,
+                         float amplitude, const int32_t* pos_start, int32_t dtype, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,6 +33,10 @@ DATA_BITS = {1: "negative length", 2: "length > max_len", 4: "sum of lengths != 
              8: "qkt_cap exceeded", 16: "av_cap exceeded", 32: "score buffer too small"}
 RAG_VGEMM_TILE_M, RAG_VGEMM_TILE_N = 128, 256
 RAG_VGEMM_MAX_BATCH, RAG_VGEMM_MAX_DIM, RAG_VGEMM_MAX_TILES = 4096, 65536, 1 << 30
+RAG_NORM_MAX_DIM = 16384
+RAG_ROTARY_HALF, RAG_ROTARY_INTERLEAVED, RAG_ROTARY_INVERSE = 0, 1, 2
+RAG_ROTARY_PLAIN, RAG_ROTARY_LINEAR, RAG_ROTARY_NTK, RAG_ROTARY_YARN = 0, 1, 2, 3
+RAG_ROTARY_MAX_DIM = 512
 VGEMM_DATA_BITS = {1: "negative size", 2: "size > RAG_VGEMM_MAX_DIM", 4: "tile_cap exceeded",
                    8: "operand buffer too small", 16: "bf16 needs k % 64 == 0 and n % 8 == 0"}
 
@@ -89,6 +93,10 @@ _c_linear = _sig("packed_linear", [_p, _i32, _p, _p, _p, _i32, _i32, _p, _i32, _
 _c_layernorm = _sig("packed_layernorm", [_p, _i32, _p, _p, _f32, _p, _i32, _i32, _i32, _i32, _p])
 _c_rmsnorm = _sig("packed_rmsnorm", [_p, _i32, _p, _i32, _p, _f32, _p, _i32, _p, _i32, _p, _i32, _p, _i32, _i32, _i32, _p])
 _c_quantize_i8 = _sig("packed_quantize_i8", [_p, _i32, _p, _i32, _p, _i32, _i32, _i32, _p])
+_f64 = ctypes.c_double
+_c_rotary_frequencies = _sig("rotary_frequencies", [_i32, _f64, _i32, _f64, _i32, _f64, _f64, _p, _p])
+_c_rotary = _sig("packed_rotary", [ctypes.POINTER(RagPlan), _p, _i32, _p, _i32, _i32, _i32, _i32, _i32, _p, _f32, _p,
+                                   _i32, _p])
 _c_vgemm_capacity = _sig("vgemm_plan_capacity", [_i32, _i32, _i32, ctypes.POINTER(_i64)])
 _c_vgemm_tile_count = _sig("vgemm_tile_count", [_i32, _p, ctypes.POINTER(_i64)])
 _c_vgemm_offsets = _sig("vgemm_offsets", [ctypes.POINTER(RagVgemmPlan), _p])
@@ -293,6 +301,30 @@ def packed_quantize_i8(x, q, scale, stream=None):
     _vector("scale", scale, T, torch.float32)
     _check("packed_quantize_i8", _c_quantize_i8(_ptr(x), _ld(x), _ptr(q), _ld(q), _ptr(scale), T, d, _dtype_code(x),
                                                 _stream(stream)))
+
+
+def rotary_frequencies(rot_dim, base=10000.0, scaling=RAG_ROTARY_PLAIN, factor=1.0, orig_len=0, beta_fast=32.0,
+                       beta_slow=1.0):
+    """(angle per position of each of rot_dim / 2 pairs, a float64 tensor on the CPU; amplitude)."""
+    f = torch.empty(max(rot_dim // 2, 1), dtype=torch.float64)
+    a = _f64()
+    _check("rotary_frequencies", _c_rotary_frequencies(rot_dim, base, scaling, factor, orig_len, beta_fast, beta_slow,
+                                                       _ptr(f), ctypes.addressof(a)))
+    return f, a.value
+
+
+def packed_rotary(plan: Plan, x, y, inv_freq, heads, head_dim=RAG_HEAD_DIM, layout=RAG_ROTARY_HALF, amplitude=1.0,
+                  pos_start=None, inverse=False, stream=None):
+    """Turns the first 2 * len(inv_freq) channels of each of `heads` heads of x [T, heads * head_dim] into y (which
+    may be x).  inv_freq is a float64 device tensor; pos_start int32 [B] holds each sequence's first position;
+    `inverse` turns back."""
+    _like("x", x, (plan.total_tokens, heads * head_dim), x.dtype)
+    _like("y", y, x.shape, x.dtype)
+    _vector("inv_freq", inv_freq, inv_freq.numel(), torch.float64)
+    _vector("pos_start", pos_start, plan.batch, torch.int32)
+    _check("packed_rotary", _c_rotary(plan.ref(), _ptr(x), _ld(x), _ptr(y), _ld(y), heads, head_dim,
+                                      2 * inv_freq.numel(), layout | (RAG_ROTARY_INVERSE if inverse else 0),
+                                      _ptr(inv_freq), amplitude, _ptr(pos_start), _dtype_code(x), _stream(stream)))
 
 
 def encoder_layer_workspace(total_tokens, max_len, d_model, heads, d_ff, dtype=RAG_BF16, flags=0):

@@ -2,6 +2,7 @@
 // Nothing here allocates device memory; every buffer comes from the caller.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstdarg>
@@ -704,6 +705,74 @@ rag_status packed_quantize_i8(const void* x, int32_t ldx, int8_t* q, int32_t ldq
         return fail(RAG_ERR_ARG, "%s: x, q and scale overlap", fn);
     hipStream_t s = static_cast<hipStream_t>(stream);
     return finish(rag::launch_quantize_i8(dtype, x, ldx, q, ldq, scale, T, d, s), s, nullptr, fn);
+}
+
+rag_status rotary_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, int32_t orig_len,
+                              double beta_fast, double beta_slow, double* inv_freq, double* amplitude) {
+    const char* fn = "rotary_frequencies";
+    if (!inv_freq || !amplitude) return fail(RAG_ERR_ARG, "%s: output pointer is NULL", fn);
+    if (rot_dim < 2 || rot_dim > RAG_ROTARY_MAX_DIM || rot_dim % 2 != 0)
+        return fail(RAG_ERR_SHAPE, "%s: rot_dim %d must be even and in [2, %d]", fn, rot_dim, RAG_ROTARY_MAX_DIM);
+    if (!(base > 1.0) || !std::isfinite(base)) return fail(RAG_ERR_ARG, "%s: base must be finite and above 1", fn);
+    if (scaling < RAG_ROTARY_PLAIN || scaling > RAG_ROTARY_YARN) return fail(RAG_ERR_ARG, "%s: bad scaling %d", fn, scaling);
+    if (scaling != RAG_ROTARY_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor)))
+        return fail(RAG_ERR_ARG, "%s: factor must be finite and at least 1", fn);
+    if (scaling == RAG_ROTARY_YARN &&
+        (orig_len < 1 || !(beta_slow > 0.0) || !(beta_fast >= beta_slow) || !std::isfinite(beta_fast)))
+        return fail(RAG_ERR_ARG, "%s: needs orig_len >= 1 and beta_fast >= beta_slow > 0", fn);
+    if (scaling == RAG_ROTARY_NTK && rot_dim > 2) base *= std::pow(factor, (double)rot_dim / (rot_dim - 2));
+    if (!std::isfinite(base)) return fail(RAG_ERR_ARG, "%s: the scaled base is not finite", fn);
+    *amplitude = 1.0;
+    double lo = 0.0, hi = 0.0;
+    if (scaling == RAG_ROTARY_YARN) {
+        // pair i turns orig_len * base^(-2i / rot_dim) / (2 pi) times over the original length;
+        // the pairs that turn beta times, as real numbers
+        const double two_pi = 6.283185307179586477, per = 0.5 * rot_dim / std::log(base);
+        lo = std::max(std::floor(per * std::log(orig_len / (beta_fast * two_pi))), 0.0);
+        hi = std::min(std::ceil(per * std::log(orig_len / (beta_slow * two_pi))), rot_dim - 1.0);
+        *amplitude = 0.1 * std::log(factor) + 1.0;
+    }
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        const double f = std::pow(base, -2.0 * i / rot_dim);
+        inv_freq[i] = scaling == RAG_ROTARY_LINEAR ? f / factor : f;
+        if (scaling == RAG_ROTARY_YARN) {
+            const double ramp = std::min(std::max((i - lo) / std::max(hi - lo, 0.001), 0.0), 1.0);
+            inv_freq[i] = f * (1.0 - ramp) + f / factor * ramp;
+        }
+    }
+    return RAG_OK;
+}
+
+rag_status packed_rotary(const rag_plan* plan, const void* x, int32_t ldx, void* y, int32_t ldy, int32_t heads,
+                         int32_t head_dim, int32_t rot_dim, int32_t layout, const double* inv_freq, float amplitude,
+                         const int32_t* pos_start, int32_t dtype, void* stream) {
+    const char* fn = "packed_rotary";
+    rag::PlanView v;
+    rag_status st;
+    if ((st = view_plan(plan, v, fn)) || (st = check_dtype(dtype, fn))) return st;
+    if (heads < 1) return fail(RAG_ERR_ARG, "%s: heads %d out of range", fn, heads);
+    if (layout < 0 || layout > (RAG_ROTARY_INTERLEAVED | RAG_ROTARY_INVERSE)) return fail(RAG_ERR_ARG, "%s: bad layout %d", fn, layout);
+    if (rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > head_dim || head_dim > RAG_ROTARY_MAX_DIM)
+        return fail(RAG_ERR_SHAPE, "%s: rot_dim %d must be even and in [2, head_dim], head_dim %d at most %d", fn, rot_dim,
+                    head_dim, RAG_ROTARY_MAX_DIM);
+    if ((int64_t)heads * head_dim > (1 << 26)) return fail(RAG_ERR_SHAPE, "%s: %d heads of %d are too wide", fn, heads, head_dim);
+    if (!std::isfinite(amplitude)) return fail(RAG_ERR_ARG, "%s: amplitude is not finite", fn);
+    if (plan->total_tokens == 0) return RAG_OK;  // nothing is read or written
+    const int64_t width = (int64_t)heads * head_dim, es = (int64_t)elem_size(dtype);
+    if ((st = check_operand(x, ldx, width, dtype, es, "x", fn)) || (st = check_operand(y, ldy, width, dtype, es, "y", fn)))
+        return st;
+    if (!inv_freq || !aligned(inv_freq, 8)) return fail(RAG_ERR_ARG, "%s: inv_freq NULL or misaligned", fn);
+    if (!aligned(pos_start, 4)) return fail(RAG_ERR_ARG, "%s: pos_start misaligned", fn);
+    const int64_t T = plan->total_tokens;
+    const Span sx{x, span_bytes(T, ldx, width, dtype), ldx}, sy{y, span_bytes(T, ldy, width, dtype), ldy};
+    if (clash(sy, sx)) return fail(RAG_ERR_ARG, "%s: y partially overlaps x", fn);
+    if (ranges_overlap(sy.p, sy.n, inv_freq, 4 * rot_dim) ||
+        (pos_start && ranges_overlap(sy.p, sy.n, pos_start, 4 * (size_t)plan->batch)))
+        return fail(RAG_ERR_ARG, "%s: y overlaps inv_freq or pos_start", fn);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return finish(rag::launch_rotary(v, dtype, x, ldx, y, ldy, heads, head_dim, rot_dim, !(layout & RAG_ROTARY_INTERLEAVED),
+                                     (layout & RAG_ROTARY_INVERSE) != 0, inv_freq, amplitude, pos_start, s),
+                  s, plan->status, fn);
 }
 
 }  // extern "C"

@@ -85,4 +85,9 @@ hipError_t launch_rmsnorm(int dtype, const void* x, int ldx, const void* residua
 hipError_t launch_quantize_i8(int dtype, const void* x, int ldx, int8_t* q, int ldq, float* scale, int T, int d,
                               hipStream_t s);
 
+// Rotary positions of the plan's tokens; inv_freq (fp64) and pos_start are device memory.
+hipError_t launch_rotary(const PlanView& p, int dtype, const void* x, int ldx, void* y, int ldy, int heads, int head_dim,
+                         int rot_dim, bool half, bool inverse, const double* inv_freq, float amplitude,
+                         const int32_t* pos_start, hipStream_t s);
+
 }  // namespace rag

@@ -45,3 +45,17 @@ def gelu(y, act):
     if act == 2:
         return 0.5 * y * (1.0 + torch.tanh(math.sqrt(2.0 / math.pi) * (y + 0.044715 * y ** 3)))
     return y
+
+
+def rotary(x, pos, freq, amplitude, heads, head_dim, half, inverse=False):
+    """Complex multiplication of each pair, float64; pos [T], freq [rot_dim / 2] float64."""
+    T, P = x.shape[0], freq.numel()
+    y = x.double().reshape(T, heads, head_dim).clone()
+    a, b = (y[..., :P], y[..., P:2 * P]) if half else (y[..., 0:2 * P:2], y[..., 1:2 * P:2])
+    angle = pos.double()[:, None] * freq
+    z = torch.complex(a, b) * torch.polar(torch.full_like(angle, amplitude), -angle if inverse else angle)[:, None]
+    if half:
+        y[..., :P], y[..., P:2 * P] = z.real, z.imag
+    else:
+        y[..., 0:2 * P:2], y[..., 1:2 * P:2] = z.real, z.imag
+    return y.reshape(T, heads * head_dim)

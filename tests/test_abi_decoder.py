@@ -85,3 +85,32 @@ def test_binding_refuses_other_shapes_and_types():
         rag.packed_rmsnorm(x, g[:32], x)
     with pytest.raises(ValueError):
         rag.packed_quantize_i8(x, q[:, :32], s)
+
+
+ROTARY = ("plan", "x", "ldx", "y", "ldy", "heads", "head_dim", "rot_dim", "layout", "inv_freq", "amplitude", "pos_start",
+          "dtype", "stream")
+
+
+def plan(**over):
+    import paper_2110_10221_amd as rag
+
+    f = dict(batch=4, total_tokens=232, max_len=128, heads=8, qkt_cap=100, av_cap=100, lengths=A + 50 * MB,
+             tok_off=A + 51 * MB, att_off=A + 52 * MB, order=A + 53 * MB, tok_seq=A + 54 * MB, qkt_item_off=A + 55 * MB,
+             av_item_off=A + 56 * MB, qkt_items=A + 57 * MB, av_items=A + 58 * MB, status=A + 59 * MB)
+    f.update(over)
+    return ctypes.byref(rag.RagPlan(**f))
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(plan=None), ARG), (dict(dtype=3), DTYPE), (dict(heads=0), ARG), (dict(heads=1 << 20), SHAPE), (dict(layout=4), ARG),
+    (dict(layout=-1), ARG), (dict(rot_dim=0), SHAPE), (dict(rot_dim=33), SHAPE), (dict(rot_dim=66), SHAPE),
+    (dict(head_dim=514, ldx=9000, ldy=9000), SHAPE), (dict(amplitude=float("inf")), ARG), (dict(x=None), ARG),
+    (dict(y=None), ARG), (dict(ldx=1023), SHAPE), (dict(ldy=1000), SHAPE), (dict(x=A + 1), SHAPE), (dict(inv_freq=None), ARG),
+    (dict(inv_freq=A + 2 * MB + 4), ARG), (dict(pos_start=A + 3 * MB + 2), ARG), (dict(y=A + 2048), ARG),
+    (dict(y=A, ldy=1040), ARG), (dict(inv_freq=A + MB), ARG), (dict(pos_start=A + MB + 4), ARG),
+    (dict(dtype=F32, x=A + 2), SHAPE)])
+def test_rotary_refuses(over, status):
+    ok = dict(plan=plan(), x=A, ldx=1024, y=A + MB, ldy=1024, heads=16, head_dim=64, rot_dim=32, layout=0,
+              inv_freq=A + 2 * MB, amplitude=1.0, pos_start=A + 3 * MB, dtype=BF16, stream=None)
+    assert call("packed_rotary", ROTARY, ok, **over) == status
+    assert call("packed_rotary", ROTARY, ok, plan=plan(total_tokens=0), x=None, y=None, inv_freq=None) == 0
