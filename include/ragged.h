@@ -530,6 +530,23 @@ rag_status packed_rotary(const rag_plan* plan, const void* x, int32_t ldx, void*
                          int32_t head_dim, int32_t rot_dim, int32_t layout, const double* inv_freq,
                          float amplitude, const int32_t* pos_start, int32_t dtype, void* stream);
 
+/*
+ * packed_linear on 8-bit rows:
+ *   y[t][n] = act(x_scale[t] * w_scale[n] * sum_k x[t][k] * w[n][k] + bias[n]) + residual[t][n]
+ * x int8 [T, K] (ldx), w int8 [N, K] contiguous, x_scale fp32 [T], w_scale fp32 [N];
+ * bias [N] or NULL, residual [T, N] (ldr) or NULL and y [T, N] (ldy) in dtype.  K % 16
+ * == 0 and K <= RAG_I8_MAX_K (the int32 sums cannot overflow), N % 8 == 0; x and w are
+ * 16-byte aligned, ldx is a multiple of 16 below 2^22; bias, residual and y are
+ * 16-byte aligned with rows that are multiples of 16 bytes.  Any int8 values are taken, -128
+ * among them.  y may equal residual (same ld) and overlaps nothing otherwise.  With
+ * T == 0 nothing is accessed and the data pointers may be NULL.
+ */
+#define RAG_I8_MAX_K 131056
+rag_status packed_linear_i8(const int8_t* x, int32_t ldx, const float* x_scale, const int8_t* w,
+                            const float* w_scale, const void* bias, const void* residual, int32_t ldr,
+                            int32_t act, void* y, int32_t ldy, int32_t T, int32_t K, int32_t N, int32_t dtype,
+                            void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -34,6 +34,7 @@ DATA_BITS = {1: "negative length", 2: "length > max_len", 4: "sum of lengths != 
 RAG_VGEMM_TILE_M, RAG_VGEMM_TILE_N = 128, 256
 RAG_VGEMM_MAX_BATCH, RAG_VGEMM_MAX_DIM, RAG_VGEMM_MAX_TILES = 4096, 65536, 1 << 30
 RAG_NORM_MAX_DIM = 16384
+RAG_I8_MAX_K = 131056
 RAG_ROTARY_HALF, RAG_ROTARY_INTERLEAVED, RAG_ROTARY_INVERSE = 0, 1, 2
 RAG_ROTARY_PLAIN, RAG_ROTARY_LINEAR, RAG_ROTARY_NTK, RAG_ROTARY_YARN = 0, 1, 2, 3
 RAG_ROTARY_MAX_DIM = 512
@@ -93,6 +94,7 @@ _c_linear = _sig("packed_linear", [_p, _i32, _p, _p, _p, _i32, _i32, _p, _i32, _
 _c_layernorm = _sig("packed_layernorm", [_p, _i32, _p, _p, _f32, _p, _i32, _i32, _i32, _i32, _p])
 _c_rmsnorm = _sig("packed_rmsnorm", [_p, _i32, _p, _i32, _p, _f32, _p, _i32, _p, _i32, _p, _i32, _p, _i32, _i32, _i32, _p])
 _c_quantize_i8 = _sig("packed_quantize_i8", [_p, _i32, _p, _i32, _p, _i32, _i32, _i32, _p])
+_c_linear_i8 = _sig("packed_linear_i8", [_p, _i32, _p, _p, _p, _p, _p, _i32, _i32, _p, _i32, _i32, _i32, _i32, _i32, _p])
 _f64 = ctypes.c_double
 _c_rotary_frequencies = _sig("rotary_frequencies", [_i32, _f64, _i32, _f64, _i32, _f64, _f64, _p, _p])
 _c_rotary = _sig("packed_rotary", [ctypes.POINTER(RagPlan), _p, _i32, _p, _i32, _i32, _i32, _i32, _i32, _p, _f32, _p,
@@ -301,6 +303,25 @@ def packed_quantize_i8(x, q, scale, stream=None):
     _vector("scale", scale, T, torch.float32)
     _check("packed_quantize_i8", _c_quantize_i8(_ptr(x), _ld(x), _ptr(q), _ld(q), _ptr(scale), T, d, _dtype_code(x),
                                                 _stream(stream)))
+
+
+def packed_linear_i8(x, x_scale, w, w_scale, y, bias=None, residual=None, act=RAG_ACT_NONE, stream=None):
+    """y = act(x_scale w_scale (x w^T) + bias) + residual: x int8 [T, K] and w int8 [N, K] in 8-bit rows with
+    their float32 scales ([T] and [N]); bias, residual and y (which may be residual) of one type."""
+    T, K = x.shape
+    N = w.shape[0]
+    _like("x", x, (T, K), torch.int8)
+    _like("w", w, (N, K), torch.int8)
+    if not w.is_contiguous():
+        raise ValueError("w must be contiguous")
+    _vector("x_scale", x_scale, T, torch.float32)
+    _vector("w_scale", w_scale, N, torch.float32)
+    _like("y", y, (T, N), y.dtype)
+    _vector("bias", bias, N, y.dtype)
+    _like("residual", residual, (T, N), y.dtype)
+    _check("packed_linear_i8", _c_linear_i8(_ptr(x), _ld(x), _ptr(x_scale), _ptr(w), _ptr(w_scale), _ptr(bias),
+                                            _ptr(residual), 0 if residual is None else _ld(residual), act, _ptr(y),
+                                            _ld(y), T, K, N, _dtype_code(y), _stream(stream)))
 
 
 def rotary_frequencies(rot_dim, base=10000.0, scaling=RAG_ROTARY_PLAIN, factor=1.0, orig_len=0, beta_fast=32.0,

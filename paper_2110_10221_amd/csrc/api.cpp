@@ -775,4 +775,34 @@ rag_status packed_rotary(const rag_plan* plan, const void* x, int32_t ldx, void*
                   s, plan->status, fn);
 }
 
+rag_status packed_linear_i8(const int8_t* x, int32_t ldx, const float* x_scale, const int8_t* w, const float* w_scale,
+                            const void* bias, const void* residual, int32_t ldr, int32_t act, void* y, int32_t ldy,
+                            int32_t T, int32_t K, int32_t N, int32_t dtype, void* stream) {
+    const char* fn = "packed_linear_i8";
+    rag_status st;
+    if ((st = check_dtype(dtype, fn))) return st;
+    if (T < 0 || K < 1 || N < 1) return fail(RAG_ERR_ARG, "%s: T %d, K %d, N %d out of range", fn, T, K, N);
+    if (act < RAG_ACT_NONE || act > RAG_ACT_GELU_TANH) return fail(RAG_ERR_ARG, "%s: bad activation %d", fn, act);
+    if (K % 16 != 0 || K > RAG_I8_MAX_K || N % 8 != 0)
+        return fail(RAG_ERR_SHAPE, "%s: needs K %% 16 == 0, K <= %d and N %% 8 == 0 (K %d, N %d)", fn, RAG_I8_MAX_K, K, N);
+    if (T == 0) return RAG_OK;  // nothing is read or written
+    if (!x || !w || !x_scale || !w_scale) return fail(RAG_ERR_ARG, "%s: an operand or its scale is NULL", fn);
+    if (ldx < K || ldx >= (1 << 22) || ldx % 16 != 0 || !aligned(x, 16) || !aligned(w, 16))
+        return fail(RAG_ERR_SHAPE, "%s: x and w must be 16-byte aligned, ldx %d a multiple of 16 in [K, 2^22)", fn, ldx);
+    if (!aligned(x_scale, 4) || !aligned(w_scale, 16))
+        return fail(RAG_ERR_SHAPE, "%s: x_scale must be 4-byte and w_scale 16-byte aligned", fn);
+    if ((st = check_rows(y, ldy, N, dtype, "y", fn))) return st;
+    if (residual && (st = check_rows(residual, ldr, N, dtype, "residual", fn))) return st;
+    if (bias && !aligned(bias, 16)) return fail(RAG_ERR_SHAPE, "%s: bias misaligned", fn);
+    const Span sy{y, span_bytes(T, ldy, N, dtype), ldy};
+    const Span in[6] = {{x, span8(T, ldx, K), -1}, {w, span8(N, K, K), -1}, {x_scale, (size_t)T * 4, -1},
+                        {w_scale, (size_t)N * 4, -1}, {bias, (size_t)N * elem_size(dtype), -1},
+                        {residual, span_bytes(T, ldr, N, dtype), ldr}};
+    for (const Span& i : in)
+        if (clash(sy, i)) return fail(RAG_ERR_ARG, "%s: y overlaps an input (only residual may equal it, with its ld)", fn);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return finish(rag::launch_linear_i8(dtype, x, ldx, x_scale, w, w_scale, bias, residual, ldr, act, y, ldy, T, K, N, s), s,
+                  nullptr, fn);
+}
+
 }  // extern "C"

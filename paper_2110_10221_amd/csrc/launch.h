@@ -90,4 +90,9 @@ hipError_t launch_rotary(const PlanView& p, int dtype, const void* x, int ldx, v
                          int rot_dim, bool half, bool inverse, const double* inv_freq, float amplitude,
                          const int32_t* pos_start, hipStream_t s);
 
+// y = act(x_scale w_scale x w^T + bias) + residual on 8-bit rows; dtype is that of bias, residual and y.
+hipError_t launch_linear_i8(int dtype, const int8_t* x, int ldx, const float* x_scale, const int8_t* w,
+                            const float* w_scale, const void* bias, const void* residual, int ldr, int act, void* y,
+                            int ldy, int T, int K, int N, hipStream_t s);
+
 }  // namespace rag

@@ -114,3 +114,23 @@ def test_rotary_refuses(over, status):
               inv_freq=A + 2 * MB, amplitude=1.0, pos_start=A + 3 * MB, dtype=BF16, stream=None)
     assert call("packed_rotary", ROTARY, ok, **over) == status
     assert call("packed_rotary", ROTARY, ok, plan=plan(total_tokens=0), x=None, y=None, inv_freq=None) == 0
+
+
+LINEAR = ("x", "ldx", "x_scale", "w", "w_scale", "bias", "residual", "ldr", "act", "y", "ldy", "T", "K", "N", "dtype", "stream")
+LINEAR_OK = dict(x=A, ldx=512, x_scale=A + MB, w=A + 2 * MB, w_scale=A + 3 * MB, bias=A + 4 * MB, residual=A + 5 * MB, ldr=264,
+                 act=0, y=A + 6 * MB, ldy=264, T=4, K=512, N=264, dtype=BF16, stream=None)
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(dtype=7), DTYPE), (dict(T=-1), ARG), (dict(K=0), ARG), (dict(N=0), ARG), (dict(act=3), ARG), (dict(act=-1), ARG),
+    (dict(K=520), SHAPE), (dict(K=131072, ldx=131072), SHAPE), (dict(N=260), SHAPE), (dict(x=None), ARG), (dict(w=None), ARG),
+    (dict(x_scale=None), ARG), (dict(w_scale=None), ARG), (dict(ldx=496), SHAPE), (dict(ldx=520), SHAPE),
+    (dict(ldx=1 << 22), SHAPE), (dict(x=A + 8), SHAPE), (dict(w=A + 2 * MB + 4), SHAPE), (dict(x_scale=A + MB + 1), SHAPE),
+    (dict(w_scale=A + 3 * MB + 4), SHAPE), (dict(y=None), ARG), (dict(ldy=256), SHAPE), (dict(ldy=268), SHAPE),
+    (dict(y=A + 6 * MB + 8), SHAPE), (dict(residual=A + 5 * MB + 8), SHAPE), (dict(ldr=256), SHAPE),
+    (dict(bias=A + 4 * MB + 8), SHAPE), (dict(y=A), ARG), (dict(y=A + 2 * MB + 1024), ARG), (dict(y=A + 5 * MB, ldy=272), ARG),
+    (dict(y=A + 5 * MB + 528), ARG), (dict(y=A + MB), ARG), (dict(y=A + 3 * MB), ARG), (dict(y=A + 4 * MB), ARG),
+    (dict(dtype=F32, ldy=266), SHAPE)])
+def test_linear_i8_refuses(over, status):
+    assert call("packed_linear_i8", LINEAR, LINEAR_OK, **over) == status
+    assert call("packed_linear_i8", LINEAR, LINEAR_OK, T=0, x=None, w=None, y=None, x_scale=None, w_scale=None) == 0
