@@ -75,7 +75,9 @@ enum {
     RAG_DATA_TOKEN_COUNT = 4,   /* sum of L_b != total_tokens                    */
     RAG_DATA_QKT_CAP = 8,       /* more score tiles than qkt_cap                 */
     RAG_DATA_AV_CAP = 16,       /* more row blocks than av_cap                   */
-    RAG_DATA_SCORE_CAP = 32     /* H * sum L_b^2 exceeds a score buffer's capacity */
+    RAG_DATA_SCORE_CAP = 32,    /* H * sum L_b^2 exceeds a score buffer's capacity */
+    RAG_DATA_KV_RANGE = 64      /* (set by ragged_attention_window_cached) some kv_len[b] is
+                                   negative or above max_kv_len, or its rows leave the cache */
 };
 
 /*
@@ -546,6 +548,44 @@ rag_status packed_linear_i8(const int8_t* x, int32_t ldx, const float* x_scale, 
                             const float* w_scale, const void* bias, const void* residual, int32_t ldr,
                             int32_t act, void* y, int32_t ldy, int32_t T, int32_t K, int32_t N, int32_t dtype,
                             void* stream);
+
+/*
+ * Causal attention with a sliding window and first tokens that stay visible
+ * (sinks), bf16 or fp32, fused like ragged_attention: position p sees the keys
+ *   j <= p  with  j > p - window  or  j < sinks
+ * (window >= 0, sinks >= 0; a window of INT32_MAX is ragged_attention_causal's mask).
+ * A position that sees no key (window 0 and no sinks) gets zeros.  Query head h
+ * reads key head h / (H / kv_heads); H = plan->heads is a multiple of kv_heads.
+ *
+ * ragged_attention_window: k and v are the packed batch's own rows [T, kv_heads * hd].
+ * ragged_attention_window_cached: k and v are caches of kv_rows rows; sequence b's
+ * keys are rows kv_first[b] .. kv_first[b] + kv_len[b] - 1 (int64 and int32 [B], device
+ * memory; 0 <= kv_len[b] <= max_kv_len), and its L_b queries are the last L_b of those
+ * kv_len[b] positions: one per sequence for a step of single tokens.  A query before
+ * position 0 (L_b > kv_len[b]) sees nothing and gets zeros.  Sequences may
+ * share rows.  Rows outside a sequence's range are not read.  A range that leaves the
+ * cache sets RAG_DATA_KV_RANGE; the call's outputs are then unspecified.
+ *
+ * q and out are [T, H * hd]; q, k, v and out are 16-byte aligned with rows that are
+ * multiples of 16 bytes, below 2^22 elements.  Keys and values that a position does not see never
+ * reach its output, infinities and NaN among them.  `workspace` (16-byte aligned) holds at least the
+ * bytes that ragged_attention_window_workspace gives for the same host values, used when few
+ * rows over many keys are split; it needs no clearing, and calls that overlap in time
+ * need one each.  (max_kv_len is max_len for ragged_attention_window.)
+ */
+rag_status ragged_attention_window_workspace(const rag_plan* plan, int32_t max_kv_len, int32_t kv_heads,
+                                             int32_t window, int32_t sinks, int32_t dtype,
+                                             size_t* bytes /* (host) out */);
+rag_status ragged_attention_window(const rag_plan* plan, const void* q, int32_t ldq, const void* k, int32_t ldk,
+                                   const void* v, int32_t ldv, int32_t kv_heads, int32_t head_dim, float scale,
+                                   int32_t window, int32_t sinks, void* out, int32_t ldo, void* workspace,
+                                   size_t workspace_bytes, int32_t dtype, void* stream);
+rag_status ragged_attention_window_cached(const rag_plan* plan, const void* q, int32_t ldq, const void* k,
+                                          int32_t ldk, const void* v, int32_t ldv, int64_t kv_rows,
+                                          const int64_t* kv_first, const int32_t* kv_len, int32_t max_kv_len,
+                                          int32_t kv_heads, int32_t head_dim, float scale, int32_t window,
+                                          int32_t sinks, void* out, int32_t ldo, void* workspace,
+                                          size_t workspace_bytes, int32_t dtype, void* stream);
 
 #ifdef __cplusplus
 }

@@ -30,7 +30,8 @@ RAG_LAYER_BUILD_PLAN = 4
 RAG_LAYER_EVENTS = 10
 RAG_NOALLOC_SCRATCH_BYTES = 64 << 20
 DATA_BITS = {1: "negative length", 2: "length > max_len", 4: "sum of lengths != total_tokens",
-             8: "qkt_cap exceeded", 16: "av_cap exceeded", 32: "score buffer too small"}
+             8: "qkt_cap exceeded", 16: "av_cap exceeded", 32: "score buffer too small",
+             64: "keys outside the cache"}
 RAG_VGEMM_TILE_M, RAG_VGEMM_TILE_N = 128, 256
 RAG_VGEMM_MAX_BATCH, RAG_VGEMM_MAX_DIM, RAG_VGEMM_MAX_TILES = 4096, 65536, 1 << 30
 RAG_NORM_MAX_DIM = 16384
@@ -95,6 +96,13 @@ _c_layernorm = _sig("packed_layernorm", [_p, _i32, _p, _p, _f32, _p, _i32, _i32,
 _c_rmsnorm = _sig("packed_rmsnorm", [_p, _i32, _p, _i32, _p, _f32, _p, _i32, _p, _i32, _p, _i32, _p, _i32, _i32, _i32, _p])
 _c_quantize_i8 = _sig("packed_quantize_i8", [_p, _i32, _p, _i32, _p, _i32, _i32, _i32, _p])
 _c_linear_i8 = _sig("packed_linear_i8", [_p, _i32, _p, _p, _p, _p, _p, _i32, _i32, _p, _i32, _i32, _i32, _i32, _i32, _p])
+_c_window_ws = _sig("ragged_attention_window_workspace", [ctypes.POINTER(RagPlan), _i32, _i32, _i32, _i32, _i32,
+                                                          ctypes.POINTER(ctypes.c_size_t)])
+_c_window = _sig("ragged_attention_window", [ctypes.POINTER(RagPlan), _p, _i32, _p, _i32, _p, _i32, _i32, _i32, _f32, _i32,
+                                             _i32, _p, _i32, _p, ctypes.c_size_t, _i32, _p])
+_c_window_cached = _sig("ragged_attention_window_cached", [ctypes.POINTER(RagPlan), _p, _i32, _p, _i32, _p, _i32, _i64, _p,
+                                                           _p, _i32, _i32, _i32, _f32, _i32, _i32, _p, _i32, _p,
+                                                           ctypes.c_size_t, _i32, _p])
 _f64 = ctypes.c_double
 _c_rotary_frequencies = _sig("rotary_frequencies", [_i32, _f64, _i32, _f64, _i32, _f64, _f64, _p, _p])
 _c_rotary = _sig("packed_rotary", [ctypes.POINTER(RagPlan), _p, _i32, _p, _i32, _i32, _i32, _i32, _i32, _p, _f32, _p,
@@ -346,6 +354,52 @@ def packed_rotary(plan: Plan, x, y, inv_freq, heads, head_dim=RAG_HEAD_DIM, layo
     _check("packed_rotary", _c_rotary(plan.ref(), _ptr(x), _ld(x), _ptr(y), _ld(y), heads, head_dim,
                                       2 * inv_freq.numel(), layout | (RAG_ROTARY_INVERSE if inverse else 0),
                                       _ptr(inv_freq), amplitude, _ptr(pos_start), _dtype_code(x), _stream(stream)))
+
+
+def ragged_attention_window_workspace(plan: Plan, max_kv_len, window, sinks=0, kv_heads=None, dtype=torch.bfloat16):
+    """Workspace bytes of the two calls below (max_kv_len: plan.max_len for the first; may be 0)."""
+    n = ctypes.c_size_t()
+    code = {torch.bfloat16: RAG_BF16, torch.float32: RAG_F32}.get(dtype, -1)
+    _check("ragged_attention_window_workspace", _c_window_ws(plan.ref(), max_kv_len, kv_heads or plan.heads, window, sinks,
+                                                             code, ctypes.byref(n)))
+    return n.value
+
+
+def _window_operands(plan, q, k, v, out, kv_heads, head_dim, workspace):
+    _like("q", q, (plan.total_tokens, plan.heads * head_dim), q.dtype)
+    _like("out", out, q.shape, q.dtype)
+    _like("k", k, (k.shape[0], kv_heads * head_dim), q.dtype)
+    _like("v", v, k.shape, q.dtype)
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return _ptr(workspace), workspace.numel() * workspace.element_size()
+
+
+def ragged_attention_window(plan: Plan, q, k, v, out, scale, window, sinks=0, kv_heads=None, head_dim=RAG_HEAD_DIM,
+                            workspace=None, stream=None):
+    """Causal attention over the packed batch: position p sees keys j <= p with j > p - window or j < sinks.
+    k and v hold kv_heads (default: all) heads, each shared by plan.heads / kv_heads query heads."""
+    kvh = kv_heads or plan.heads
+    ws, n = _window_operands(plan, q, k, v, out, kvh, head_dim, workspace)
+    _like("k", k, (plan.total_tokens, kvh * head_dim), q.dtype)
+    _check("ragged_attention_window", _c_window(plan.ref(), _ptr(q), _ld(q), _ptr(k), _ld(k), _ptr(v), _ld(v), kvh,
+                                                head_dim, scale, window, sinks, _ptr(out), _ld(out), ws, n,
+                                                _dtype_code(q), _stream(stream)))
+
+
+def ragged_attention_window_cached(plan: Plan, q, k, v, kv_first, kv_len, max_kv_len, out, scale, window, sinks=0,
+                                   kv_heads=None, head_dim=RAG_HEAD_DIM, workspace=None, stream=None):
+    """The same over caches k and v [rows, kv_heads * head_dim]: sequence b's keys are the kv_len[b] rows from
+    kv_first[b] (int32 and int64 device tensors), its queries the last plan.lengths[b] of those positions."""
+    kvh = kv_heads or plan.heads
+    ws, n = _window_operands(plan, q, k, v, out, kvh, head_dim, workspace)
+    _vector("kv_first", kv_first, plan.batch, torch.int64)
+    _vector("kv_len", kv_len, plan.batch, torch.int32)
+    _check("ragged_attention_window_cached", _c_window_cached(
+        plan.ref(), _ptr(q), _ld(q), _ptr(k), _ld(k), _ptr(v), _ld(v), k.shape[0], _ptr(kv_first), _ptr(kv_len), max_kv_len,
+        kvh, head_dim, scale, window, sinks, _ptr(out), _ld(out), ws, n, _dtype_code(q), _stream(stream)))
 
 
 def encoder_layer_workspace(total_tokens, max_len, d_model, heads, d_ff, dtype=RAG_BF16, flags=0):

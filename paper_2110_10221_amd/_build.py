@@ -17,7 +17,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libragged.so")
 OBJ_DIR = os.path.join(ROOT, "_build", "ragged")
 
-SOURCES = ["api.cpp", "offsets.hip", "attention.hip", "gemm.hip", "gemm_f32.hip", "gemm_small.hip", "gemm_big.hip", "gemm_i8.hip",
+SOURCES = ["api.cpp", "offsets.hip", "attention.hip", "attention_window.hip", "gemm.hip", "gemm_f32.hip", "gemm_small.hip", "gemm_big.hip", "gemm_i8.hip",
            "layernorm.hip", "rmsnorm.hip", "rotary.hip", "noalloc.hip"]
 ARCH = "gfx950"
 

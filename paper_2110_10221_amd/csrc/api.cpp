@@ -805,4 +805,95 @@ rag_status packed_linear_i8(const int8_t* x, int32_t ldx, const float* x_scale, 
                   nullptr, fn);
 }
 
+namespace {
+
+constexpr int32_t kWindowMaxLd = 1 << 22;  // 32 rows of a chunk in 32-bit byte offsets
+
+rag_status check_window(const rag_plan* plan, rag::PlanView& v, int32_t max_kv_len, int32_t kv_heads, int32_t window,
+                        int32_t sinks, int32_t dtype, const char* fn) {
+    rag_status st;
+    if ((st = view_plan(plan, v, fn)) || (st = check_dtype(dtype, fn))) return st;
+    if (kv_heads < 1 || plan->heads % kv_heads != 0)
+        return fail(RAG_ERR_SHAPE, "%s: %d heads are not a multiple of %d key heads", fn, plan->heads, kv_heads);
+    if (window < 0 || sinks < 0 || max_kv_len < 0)
+        return fail(RAG_ERR_ARG, "%s: window %d, sinks %d, max_kv_len %d out of range", fn, window, sinks, max_kv_len);
+    if (((int64_t)plan->total_tokens + RAG_TILE) * (plan->heads / kv_heads) > INT32_MAX)
+        return fail(RAG_ERR_SHAPE, "%s: tokens * heads per key head exceed 2^31 - 1", fn);
+    return RAG_OK;
+}
+
+rag_status window_impl(const rag_plan* plan, const void* q, int32_t ldq, const void* k, int32_t ldk, const void* vv,
+                       int32_t ldv, const rag::WindowKeys& keys, int32_t kv_heads, int32_t head_dim, float scale,
+                       int32_t window, int32_t sinks, void* out, int32_t ldo, void* workspace, size_t workspace_bytes,
+                       int32_t dtype, void* stream, const char* fn) {
+    rag::PlanView v;
+    rag_status st;
+    if ((st = check_window(plan, v, keys.max_len, kv_heads, window, sinks, dtype, fn))) return st;
+    if (head_dim != RAG_HEAD_DIM) return fail(RAG_ERR_SHAPE, "%s: head_dim %d unsupported (only %d)", fn, head_dim, RAG_HEAD_DIM);
+    if (!std::isfinite(scale)) return fail(RAG_ERR_ARG, "%s: scale is not finite", fn);
+    const int64_t T = plan->total_tokens, wq = (int64_t)plan->heads * head_dim, wk = (int64_t)kv_heads * head_dim;
+    if (T == 0) return RAG_OK;  // nothing is read or written
+    if ((st = check_rows(q, ldq, wq, dtype, "q", fn)) || (st = check_rows(out, ldo, wq, dtype, "out", fn))) return st;
+    if (keys.rows > 0 &&
+        ((st = check_rows(k, ldk, wk, dtype, "k", fn)) || (st = check_rows(vv, ldv, wk, dtype, "v", fn)))) return st;
+    if (ldq >= kWindowMaxLd || ldk >= kWindowMaxLd || ldv >= kWindowMaxLd || ldo >= kWindowMaxLd)
+        return fail(RAG_ERR_SHAPE, "%s: a leading dimension is not below %d", fn, kWindowMaxLd);
+    const int splits = rag::window_splits(T, plan->batch, plan->heads, kv_heads, plan->max_len, keys.max_len, window, sinks);
+    const size_t need = rag::window_workspace(T, plan->heads, splits);
+    if (need > 0) {
+        if (workspace_bytes < need)
+            return fail(RAG_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, workspace_bytes, need);
+        if (!workspace || !aligned(workspace, 16)) return fail(RAG_ERR_ARG, "%s: workspace NULL or misaligned", fn);
+    }
+    const Span so{out, span_bytes(T, ldo, wq, dtype), ldo}, sw{need ? workspace : nullptr, need, -2};
+    const Span in[5] = {{q, span_bytes(T, ldq, wq, dtype), -1}, {k, span_bytes(keys.rows, ldk, wk, dtype), -1},
+                        {vv, span_bytes(keys.rows, ldv, wk, dtype), -1},
+                        {keys.first, keys.first ? 8 * (size_t)plan->batch : 0, -1}, {keys.len, keys.len ? 4 * (size_t)plan->batch : 0, -1}};
+    for (const Span& i : in)
+        if (clash(so, i) || clash(sw, i)) return fail(RAG_ERR_ARG, "%s: out or the workspace overlaps an input", fn);
+    if (clash(so, sw)) return fail(RAG_ERR_ARG, "%s: out overlaps the workspace", fn);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return finish(rag::launch_attention_window(v, dtype, q, ldq, k, ldk, vv, ldv, keys, kv_heads, scale, window, sinks, out,
+                                               ldo, splits, need ? workspace : nullptr, s),
+                  s, plan->status, fn);
+}
+
+}  // namespace
+
+rag_status ragged_attention_window_workspace(const rag_plan* plan, int32_t max_kv_len, int32_t kv_heads, int32_t window,
+                                             int32_t sinks, int32_t dtype, size_t* bytes) {
+    const char* fn = "ragged_attention_window_workspace";
+    rag::PlanView v;
+    if (!bytes) return fail(RAG_ERR_ARG, "%s: output pointer is NULL", fn);
+    const rag_status st = check_window(plan, v, max_kv_len, kv_heads, window, sinks, dtype, fn);
+    if (st) return st;
+    *bytes = rag::window_workspace(plan->total_tokens, plan->heads,
+                                   rag::window_splits(plan->total_tokens, plan->batch, plan->heads, kv_heads, plan->max_len,
+                                                      max_kv_len, window, sinks));
+    return RAG_OK;
+}
+
+rag_status ragged_attention_window(const rag_plan* plan, const void* q, int32_t ldq, const void* k, int32_t ldk,
+                                   const void* v, int32_t ldv, int32_t kv_heads, int32_t head_dim, float scale,
+                                   int32_t window, int32_t sinks, void* out, int32_t ldo, void* workspace,
+                                   size_t workspace_bytes, int32_t dtype, void* stream) {
+    const rag::WindowKeys keys{nullptr, nullptr, plan ? plan->total_tokens : 0, plan ? plan->max_len : 0};
+    return window_impl(plan, q, ldq, k, ldk, v, ldv, keys, kv_heads, head_dim, scale, window, sinks, out, ldo, workspace,
+                       workspace_bytes, dtype, stream, "ragged_attention_window");
+}
+
+rag_status ragged_attention_window_cached(const rag_plan* plan, const void* q, int32_t ldq, const void* k, int32_t ldk,
+                                          const void* v, int32_t ldv, int64_t kv_rows, const int64_t* kv_first,
+                                          const int32_t* kv_len, int32_t max_kv_len, int32_t kv_heads, int32_t head_dim,
+                                          float scale, int32_t window, int32_t sinks, void* out, int32_t ldo,
+                                          void* workspace, size_t workspace_bytes, int32_t dtype, void* stream) {
+    const char* fn = "ragged_attention_window_cached";
+    if (kv_rows < 0 || kv_rows > ((int64_t)1 << 40)) return fail(RAG_ERR_ARG, "%s: kv_rows %lld out of range", fn, (long long)kv_rows);
+    if (!kv_first || !kv_len || !aligned(kv_first, 8) || !aligned(kv_len, 4))
+        return fail(RAG_ERR_ARG, "%s: kv_first or kv_len NULL or misaligned", fn);
+    const rag::WindowKeys keys{kv_first, kv_len, kv_rows, max_kv_len};
+    return window_impl(plan, q, ldq, k, ldk, v, ldv, keys, kv_heads, head_dim, scale, window, sinks, out, ldo, workspace,
+                       workspace_bytes, dtype, stream, fn);
+}
+
 }  // extern "C"

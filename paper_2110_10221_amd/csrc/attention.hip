@@ -20,7 +20,7 @@
 #include <algorithm>
 #include <cfloat>
 
-#include "device_common.h"
+#include "attention_common.h"
 #include "launch.h"
 
 namespace rag {
@@ -52,19 +52,9 @@ __device__ __forceinline__ bool plan_ok(const PlanArgs& pa, int64_t score_cap) {
     return true;
 }
 
-__device__ __forceinline__ u32x4 ld16(const uint16_t* p) { return *reinterpret_cast<const u32x4*>(p); }
-
 // ---------------------------------------------------------------------------
 // QK^T
 // ---------------------------------------------------------------------------
-
-// Element offset of (row, col) in [rows][64 channels] LDS storage (128-byte rows,
-// two per 256-byte bank line) whose 16-byte chunks are XOR-swizzled by row bits
-// 1-3: the K-operand reads (16 consecutive rows, one chunk each) then meet 16
-// distinct bank groups, and in the transposed V reads (rows r..r+3, four
-// adjacent chunks each) rows r and r+2 use opposite halves of the row.
-__device__ __forceinline__ int kv_swz(int row) { return (((row >> 1) & 1) << 2) | ((row >> 2) & 3); }
-__device__ __forceinline__ int kv_off(int row, int col) { return row * kHeadDim + ((((col >> 3) ^ kv_swz(row)) & 7) << 3) + (col & 7); }
 
 // The bf16 operators take one work item per (sequence, 64-query block, group of
 // G consecutive heads), G a divisor of H chosen at launch so that the batch
@@ -738,32 +728,11 @@ __global__ __launch_bounds__(256) void k_attn_v_f32(PlanArgs pa, const float* __
 // K / V rows in that XCD's L2), the runs round-robin.
 // ---------------------------------------------------------------------------
 
-constexpr float kSumCap = 65536.f;  // largest lane sum of a chunk's exponentials kept (2^16)
 constexpr int kStreamWaves = 2, kStreamThreads = kStreamWaves * kWave;
 constexpr int kStreamBlocks = 4 / kStreamWaves;                 // 1 KB copies of K (and of V) per wave and chunk
 constexpr int kStreamChunk = 32;                                // keys per LDS stage
 constexpr int kStreamStageElems = 2 * kStreamChunk * kHeadDim;  // K rows, then V rows
-constexpr int kStreamRun = 8;
 constexpr int kStreamPerCu = 64;  // grid cap in workgroups per CU (they then loop over the list)
-
-__device__ __forceinline__ int stream_item(int bid, int nb) {  // nb: a multiple of 8 * kStreamRun
-    const int xcd = bid % 8, j = bid / 8;
-    return ((j / kStreamRun) * 8 + xcd) * kStreamRun + j % kStreamRun;
-}
-
-__device__ __forceinline__ void attn_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-
-// Combine a value with the one held by the lane 32 apart (the other half of
-// the same query row): v_permlane32_swap hands each half the other's value.
-__device__ __forceinline__ float max_xor32(float v) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-
-__device__ __forceinline__ float sum_xor32(float v) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
 
 // KS = 2: two wave pairs per item, each walking half of the item's key chunks in LDS stages
 // of its own; the pairs' (reference, sum, output) states meet in LDS at the end.

@@ -1,0 +1,470 @@
+// Causal attention with a sliding window and first tokens that stay visible, over the
+// packed batch or over a cache: position p sees the keys j <= p with j > p - window or
+// j < sinks.
+//
+// One pass over the keys that some row of an item sees, like the fused ragged attention
+// (attention.hip): chunks of 32 keys through two LDS stages, S^T = K Q^T in fp32, a running
+// reference m and sum of the softmax, O^T += V^T E^T, one division at the end.
+//   items   the entries of the plan's Attn.V list, 64 rows per workgroup of two waves.  A
+//           row is a (token, query head) pair: the G heads that share a key head
+//           are consecutive rows, so their keys are read once and a step of
+//           single tokens fills rows with heads.  Entry (b, h, ti) is tile (h % G) *
+//           ceil(L_b / 64) + ti of key head h / G; tiles past the last row return.
+//   chunks  of a tile: those of the window from the last to the first, then the sinks'.
+//           Downwards because a row's own key is always visible: the first chunk then
+//           sets nearly every row's reference, where upwards the rows whose
+//           window begins later would raise theirs from nothing, a recomputation each tile.
+//   masks   only in chunks that cut some row's range; a chunk no row of a wave sees is
+//           skipped by it.  Hidden values are multiplied by a zero, so one that is not
+//           finite is taken out of the operand there and added to the rows that see it.
+//   splits  where few rows meet many keys the chunks are dealt to several workgroups
+//           (blockIdx.y), whose (reference, sum, output) states a second launch joins.
+// bf16 rounds the unnormalised exponentials to bf16 for the P V product (a relative 2^-9 of each
+// of many terms, against 2^-9 of the stored result) and nothing else; fp32
+// products run on v_mfma_f32_32x32x2f32 and round nothing.
+#include <algorithm>
+#include <cfloat>
+#include <type_traits>
+
+#include "attention_common.h"
+#include "launch.h"
+
+namespace rag {
+namespace {
+
+constexpr int kWinWaves = 2, kWinThreads = kWinWaves * kWave;
+constexpr int kWinChunk = 32;       // keys per LDS stage
+constexpr int kWinPerCu = 64;       // grid cap in workgroups per CU
+
+struct WinArgs {
+    const int32_t* lengths;
+    const int32_t* tok_off;
+    const int32_t* av_items;
+    int32_t* status;
+    const int64_t* kv_first;  // NULL: the packed batch's own rows
+    const int32_t* kv_len;
+    int64_t kv_rows;
+    int max_kv;
+    const void *q, *k, *v;
+    void* out;
+    int ldq, ldk, ldv, ldo;
+    int heads, group;  // query heads; query heads per key head
+    int window, sinks;
+    float scale;
+    int T, splits;
+    float* part_o;   // [splits][T][heads][64] unnormalised outputs
+    float* part_ml;  // [splits][T][heads][2] reference and sum
+};
+
+template <bool BF16>
+struct WinT;
+template <>
+struct WinT<true> {
+    using T = uint16_t;
+    static constexpr int kRow = 128, kChunks = 8;  // bytes and 16-byte chunks of a row
+    static __device__ __forceinline__ int swz(int row) { return kv_swz(row); }
+};
+template <>
+struct WinT<false> {
+    using T = float;
+    static constexpr int kRow = 256, kChunks = 16;
+    static __device__ __forceinline__ int swz(int row) { return row & 15; }
+};
+
+// The last key before position p's window (keys above it are in the window), at least -1.
+__device__ __forceinline__ int window_below(int p, int window) {
+    return (int)max((int64_t)p - window, (int64_t)-1);
+}
+
+// ds_read_b64_tr_b16: within 16 lanes, lane 4 e + q addresses row e, columns 4 q .. 4 q + 3 of a
+// 4 x 16 block and receives column (lane % 16) of its rows.
+__device__ __forceinline__ u32x2 read_tr(const uint16_t* p) {
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)p));
+}
+
+__device__ __forceinline__ floatx16 mfma32x32x2(float a, float b, const floatx16& c) {
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t chunk_rsrc(const void* base, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
+}
+
+__device__ __forceinline__ void copy_1k(__amdgpu_buffer_rsrc_t r, void* dst, int off) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)dst, 16, off, 0, 0, 0);
+}
+
+__device__ __forceinline__ bool finite_f32(float v) { return fabsf(v) <= FLT_MAX; }
+
+template <bool BF16>
+__global__ __launch_bounds__(kWinThreads, BF16 ? 4 : 2)
+void k_attention_window(WinArgs a) {
+    using W = WinT<BF16>;
+    using T = typename W::T;
+    constexpr int kStage = 2 * kWinChunk * W::kRow;        // K rows, then V rows
+    constexpr int kBlockRows = 1024 / W::kRow;             // rows of a 1 KB copy
+    constexpr int kBlocks = kWinChunk / kBlockRows / kWinWaves;  // copies of K (and of V) per wave and chunk
+    constexpr int kEs = (int)sizeof(T);
+    if (a.status[0] != 0) return;
+    __shared__ __attribute__((aligned(16))) uint8_t kvs[2 * kStage];
+    const int n_items = uni(a.status[2]);
+    const int wave = uni(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const int l32 = lane % 32, h2 = lane / 32;
+    // (a zero scale would turn hidden keys' -inf into NaN; below 1e-30 every exponential is 1 anyway)
+    const float zs = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-30f);
+    const bool flip = a.scale < 0.f;
+    const int G = a.group;
+
+    for (int base = 0; base < n_items; base += gridDim.x) {
+        const int it = base + stream_item(blockIdx.x, gridDim.x);
+        if (it >= n_items) break;
+        const int b = uni(a.av_items[3 * it]), h = uni(a.av_items[3 * it + 1]), ti = uni(a.av_items[3 * it + 2]);
+        const int L = uni(a.lengths[b]), t0 = uni(a.tok_off[b]);
+        const int hk = h / G, rows = L * G;
+        const int r0 = ((h - hk * G) * ((L + kTile - 1) / kTile) + ti) * kTile;
+        if (r0 >= rows) continue;
+        int n = L;  // keys
+        int64_t first = t0;
+        if (a.kv_len) {
+            n = uni(a.kv_len[b]);
+            first = uni64(a.kv_first[b]);
+            if (n < 0 || n > a.max_kv || first < 0 || first > a.kv_rows - n) {
+                if (threadIdx.x == 0) atomicOr(a.status, kDataKvRange);
+                continue;
+            }
+        }
+        const int past = n - L;  // position of token 0
+        // the wave's rows and positions, and the tile's
+        const int w0 = r0 + wave * 32;
+        const bool active = w0 < rows;
+        const int row = min(w0 + l32, rows - 1), tok = row / G, head = hk * G + (row - tok * G);
+        const int p = past + tok, below = window_below(p, a.window);
+        const int plo = past + min(w0, rows - 1) / G, phi = past + min(w0 + 31, rows - 1) / G;
+        const int tlo = past + r0 / G, thi = past + min(r0 + kTile - 1, rows - 1) / G;
+        // chunks: window [cw0, cw1) downwards, then the sinks' [0, cs) below them
+        int cw0 = (window_below(tlo, a.window) + 1) / kWinChunk, cw1 = thi / kWinChunk + 1;
+        if (thi < 0 || a.window == 0) cw0 = cw1 = INT32_MAX / kWinChunk;
+        const int seen_sinks = min(a.sinks, thi + 1);
+        const int cs = seen_sinks > 0 ? min((seen_sinks + kWinChunk - 1) / kWinChunk, cw0) : 0;
+        const int nwin = cw1 - cw0, nch = nwin + cs;
+        const int per = (nch + a.splits - 1) / a.splits;
+        const int i0 = min(nch, (int)blockIdx.y * per), i1 = min(nch, i0 + per);
+        const auto chunk = [&](int i) { return i < nwin ? cw1 - 1 - i : cs - 1 - (i - nwin); };
+
+        // copy i of this wave fills rows 1 KB apart from block wave * kBlocks + i of K and V;
+        // rows past the last key arrive as zeros.  The descriptor starts at the chunk, so a
+        // cache of any size is in reach.
+        int vko[kBlocks], vvo[kBlocks];
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i) {
+            const int r = (wave * kBlocks + i) * kBlockRows + lane / W::kChunks;
+            const int c = ((lane % W::kChunks) ^ W::swz(r)) * 16;
+            vko[i] = r * a.ldk * kEs + c;
+            vvo[i] = r * a.ldv * kEs + c;
+        }
+        const auto issue = [&](int i, auto stg) {
+            const int k0 = chunk(i) * kWinChunk, valid = min(kWinChunk, n - k0);
+            const __amdgpu_buffer_rsrc_t rk = chunk_rsrc(
+                static_cast<const T*>(a.k) + (first + k0) * a.ldk + hk * kHeadDim, (uint32_t)valid * a.ldk * kEs);
+            const __amdgpu_buffer_rsrc_t rv = chunk_rsrc(
+                static_cast<const T*>(a.v) + (first + k0) * a.ldv + hk * kHeadDim, (uint32_t)valid * a.ldv * kEs);
+            uint8_t* const st = kvs + decltype(stg)::value * kStage;
+#pragma unroll
+            for (int i2 = 0; i2 < kBlocks; ++i2) {
+                const int blk = wave * kBlocks + i2;
+                copy_1k(rk, st + blk * 1024, vko[i2]);
+                copy_1k(rv, st + kWinChunk * W::kRow + blk * 1024, vvo[i2]);
+            }
+        };
+        // Q operand: bf16 k = 16 ks + 8 h2 .. of row l32; fp32 k = 8 u + 4 h2 + e
+        u32x4 qf[BF16 ? 4 : 8];
+        {
+            const T* const qrow = static_cast<const T*>(a.q) + (int64_t)(t0 + tok) * a.ldq + head * kHeadDim;
+#pragma unroll
+            for (int u = 0; u < (BF16 ? 4 : 8); ++u) {
+                qf[u] = active ? *reinterpret_cast<const u32x4*>(qrow + (BF16 ? 16 * u + 8 * h2 : 8 * u + 4 * h2))
+                               : u32x4{0u, 0u, 0u, 0u};
+                if (flip) qf[u] ^= BF16 ? 0x80008000u : 0x80000000u;
+            }
+        }
+        float m = -FLT_MAX, lsum = 0.f;
+        bool fresh = true;  // no chunk yet
+        floatx16 oacc[2];
+#pragma unroll
+        for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) oacc[cb][r] = 0.f;
+
+        const auto step = [&](int i, auto stg) {
+            constexpr int STG = decltype(stg)::value;
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's copies of chunk i
+            attn_barrier();  // ... and the other wave's; the other stage was last read in step i - 1
+            if (i + 1 < i1) issue(i + 1, std::integral_constant<int, 1 - STG>{});
+            const int c0 = chunk(i) * kWinChunk, c1 = c0 + kWinChunk - 1;
+            if (!active || c0 > phi || (c1 <= window_below(plo, a.window) && c0 >= a.sinks)) return;
+            // every key visible to every row?
+            const bool whole = c1 <= plo && (c0 > window_below(phi, a.window) || c1 < a.sinks);
+            const uint8_t* const kst = kvs + STG * kStage;
+            const uint8_t* const vst = kst + kWinChunk * W::kRow;
+            const auto visible = [&](int j) { return j <= p && (j > below || j < a.sinks); };
+            floatx16 acc;
+            const auto scores = [&] {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+                if constexpr (BF16) {
+                    const uint16_t* const ks = reinterpret_cast<const uint16_t*>(kst);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        acc = mfma32x32x16(as_bf16x8(*reinterpret_cast<const u32x4*>(ks + kv_off(l32, 16 * u + 8 * h2))),
+                                           as_bf16x8(qf[u]), acc);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        const floatx4 kf = *reinterpret_cast<const floatx4*>(kst + l32 * W::kRow + (((2 * u + h2) ^ W::swz(l32)) * 16));
+                        const floatx4 q4 = __builtin_bit_cast(floatx4, qf[u]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc = mfma32x32x2(kf[e], q4[e], acc);
+                    }
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (!visible(c0 + 8 * (r / 4) + 4 * h2 + (r % 4))) acc[r] = -INFINITY;
+                }
+            };
+            const auto chunk_max = [&] {
+                float cmax = acc[0];
+#pragma unroll
+                for (int r = 1; r < 16; ++r) cmax = fmaxf(cmax, acc[r]);
+                return max_xor32(cmax) * zs;
+            };
+            const auto exps = [&] {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[r] = __builtin_amdgcn_exp2f(fmaf(acc[r], zs, -m));
+                float s[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) s[r] = acc[2 * r] + acc[2 * r + 1];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[r] += s[r + 4];
+                return (s[0] + s[2]) + (s[1] + s[3]);
+            };
+            scores();
+            if (fresh) m = fmaxf(chunk_max(), -FLT_MAX);  // (no visible key: any later score is far above)
+            float ps = exps();
+            // a lane sum above kSumCap (or NaN) means a score well above m: raise m to the
+            // chunk's maximum and rescale what has been summed
+            if (!fresh && __ballot(!(ps <= kSumCap)) != 0) {
+                scores();
+                const float mn = fmaxf(m, chunk_max());
+                const float alpha = __builtin_amdgcn_exp2f(m - mn);
+                lsum *= alpha;
+#pragma unroll
+                for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) oacc[cb][r] *= alpha;
+                m = mn;
+                ps = exps();
+            }
+            fresh = false;
+            lsum += ps;
+            // values that are not finite, in a chunk with hidden keys: added to the rows that
+            // see them (a positive weight leaves an infinity or NaN what it is)
+            const auto add_seen = [&](auto value) {
+                for (int kk = 0; kk < kWinChunk; ++kk) {
+                    if (!visible(c0 + kk)) continue;
+#pragma unroll
+                    for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const float x = value(kk, 32 * cb + 8 * (r / 4) + 4 * h2 + (r % 4));
+                            if (!finite_f32(x)) oacc[cb][r] += x;
+                        }
+                }
+            };
+            if constexpr (BF16) {
+                const uint16_t* const vs = reinterpret_cast<const uint16_t*>(vst);
+                // transposed reads: lane's keys 16 t + {4 h2 .. + 3, 8 + 4 h2 .. + 3} of channel 32 cb + l32
+                const int e4 = (lane % 16) / 4, q4 = lane % 4, g4 = lane / 16;
+                u32x2 tr[2][2][2];
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+                        for (int hi = 0; hi < 2; ++hi)
+                            tr[t][cb][hi] = read_tr(vs + 16 * t * kHeadDim + kv_off(4 * (g4 >> 1) + e4 + 8 * hi, 32 * cb + 16 * (g4 & 1) + 4 * q4));
+                if (!whole) {
+                    bool bad = false;
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+                            for (int hi = 0; hi < 2; ++hi)
+#pragma unroll
+                                for (int w = 0; w < 2; ++w) {
+                                    const uint32_t x = tr[t][cb][hi][w];
+                                    bad |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+                                }
+                    if (__ballot(bad) != 0) {
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+#pragma unroll
+                            for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+                                for (int hi = 0; hi < 2; ++hi)
+#pragma unroll
+                                    for (int w = 0; w < 2; ++w) {
+                                        uint32_t x = tr[t][cb][hi][w];
+                                        if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+                                        if ((x & 0x7f800000u) == 0x7f800000u) x &= 0x0000ffffu;
+                                        tr[t][cb][hi][w] = x;
+                                    }
+                        add_seen([&](int kk, int ch) { return bf16_to_f32(vs[kv_off(kk, ch)]); });
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    u32x4 pw;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) pw[e] = pack_bf16x2(acc[8 * t + 2 * e], acc[8 * t + 2 * e + 1]);
+                    const bf16x8 pb = as_bf16x8(pw);
+#pragma unroll
+                    for (int cb = 0; cb < 2; ++cb)
+                        oacc[cb] = mfma32x32x16(
+                            as_bf16x8(u32x4{tr[t][cb][0][0], tr[t][cb][0][1], tr[t][cb][1][0], tr[t][cb][1][1]}), pb, oacc[cb]);
+                }
+            } else {
+                const auto value = [&](int kk, int ch) {
+                    return *reinterpret_cast<const float*>(vst + kk * W::kRow + (((ch >> 2) ^ W::swz(kk)) * 16) + (ch & 3) * 4);
+                };
+                float vf[2][16];
+                bool bad = false;
+#pragma unroll
+                for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        vf[cb][r] = value(8 * (r / 4) + 4 * h2 + (r % 4), 32 * cb + l32);
+                        bad |= !finite_f32(vf[cb][r]);
+                    }
+                if (!whole && __ballot(bad) != 0) {
+#pragma unroll
+                    for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            if (!finite_f32(vf[cb][r])) vf[cb][r] = 0.f;
+                    add_seen(value);
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+#pragma unroll
+                    for (int cb = 0; cb < 2; ++cb)
+                        oacc[cb] = mfma32x32x2(vf[cb][r], acc[r], oacc[cb]);
+            }
+        };
+        attn_barrier();  // both stages are free: the previous item's reads are done
+        if (i0 < i1) issue(i0, std::integral_constant<int, 0>{});
+        for (int i = i0; i < i1; i += 2) {
+            step(i, std::integral_constant<int, 0>{});
+            if (i + 1 < i1) step(i + 1, std::integral_constant<int, 1>{});
+        }
+        if (!active || w0 + l32 >= rows) continue;
+        float sum = sum_xor32(lsum);
+        const bool empty = p < 0 || (a.window == 0 && a.sinks == 0);
+        if (empty) sum = 1.f;  // (its output is zero)
+        const int64_t gr = (int64_t)(t0 + tok);
+        if (a.splits > 1) {
+            const int64_t slot = ((int64_t)blockIdx.y * a.T + gr) * a.heads + head;
+            float* const po = a.part_o + slot * kHeadDim;
+#pragma unroll
+            for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<floatx4*>(po + 32 * cb + 8 * g + 4 * h2) =
+                        floatx4{oacc[cb][4 * g], oacc[cb][4 * g + 1], oacc[cb][4 * g + 2], oacc[cb][4 * g + 3]};
+            if (h2 == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * slot) = float2{m, sum};
+        } else {
+            const float inv = 1.0f / sum;
+            T* const orow = static_cast<T*>(a.out) + gr * a.ldo + head * kHeadDim;
+#pragma unroll
+            for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float o0 = oacc[cb][4 * g] * inv, o1 = oacc[cb][4 * g + 1] * inv, o2 = oacc[cb][4 * g + 2] * inv,
+                                o3 = oacc[cb][4 * g + 3] * inv;
+                    if constexpr (BF16)
+                        *reinterpret_cast<u32x2*>(orow + 32 * cb + 8 * g + 4 * h2) = u32x2{pack_bf16x2(o0, o1), pack_bf16x2(o2, o3)};
+                    else
+                        *reinterpret_cast<floatx4*>(orow + 32 * cb + 8 * g + 4 * h2) = floatx4{o0, o1, o2, o3};
+                }
+        }
+    }
+}
+
+// Joins the splits' states of one (token, head) row per wave, a channel per lane.
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_attention_window_join(WinArgs a) {
+    if (a.status[0] != 0) return;
+    using T = typename WinT<BF16>::T;
+    const int64_t rows = (int64_t)a.T * a.heads, r = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+    const int lane = threadIdx.x % kWave;
+    if (r >= rows) return;
+    float m = -FLT_MAX;
+    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[2 * (s * rows + r)]);
+    float sum = 0.f, o = 0.f;
+    for (int s = 0; s < a.splits; ++s) {
+        const float w = __builtin_amdgcn_exp2f(a.part_ml[2 * (s * rows + r)] - m);
+        sum = fmaf(w, a.part_ml[2 * (s * rows + r) + 1], sum);
+        o = fmaf(w, a.part_o[(s * rows + r) * kHeadDim + lane], o);
+    }
+    o *= 1.0f / sum;
+    T* const dst = static_cast<T*>(a.out) + (r / a.heads) * a.ldo + (r % a.heads) * kHeadDim + lane;
+    if constexpr (BF16) *dst = f32_to_bf16(o);
+    else *dst = o;
+}
+
+}  // namespace
+
+// Workgroups over the keys of one item: as many as fill the GPU where the batch has few
+// items, each with at least kWinSplitChunks chunks of the longest row.  (Whole GPUs' 256 CUs: the
+// workspace is sized by the same rule, on the host.)
+int window_splits(int64_t T, int64_t batch, int64_t heads, int64_t kv_heads, int64_t max_len, int64_t max_kv, int64_t window,
+                  int64_t sinks) {
+    constexpr int64_t kWinSplitChunks = 8, kWant = 256 * 4;
+    if (T <= 0) return 1;
+    const int64_t group = heads / kv_heads;
+    // tiles of 64 rows that hold any; keys a tile walks: its rows' positions and window, or all
+    const int64_t tiles = kv_heads * std::min((T * group + 63 * batch) / 64, batch * ((max_len * group + 63) / 64));
+    const int64_t keys = std::min(max_kv, std::min(window, max_kv) + std::min(sinks, max_kv) + std::min<int64_t>(max_len, 64));
+    const int64_t chunks = (keys + 31) / 32;
+    return (int)std::max<int64_t>(1, std::min({kWant / std::max<int64_t>(tiles, 1), chunks / kWinSplitChunks, (int64_t)256}));
+}
+
+size_t window_workspace(int64_t T, int64_t heads, int64_t splits) {
+    return splits > 1 ? (size_t)(splits * T * heads * (kHeadDim + 2)) * sizeof(float) : 0;
+}
+
+hipError_t launch_attention_window(const PlanView& p, int dtype, const void* q, int ldq, const void* k, int ldk,
+                                   const void* v, int ldv, const WindowKeys& keys, int kv_heads, float scale, int window,
+                                   int sinks, void* out, int ldo, int splits, void* workspace, hipStream_t s) {
+    if (p.total_tokens == 0) return hipSuccess;
+    float* const ws = static_cast<float*>(workspace);
+    const int64_t rows = (int64_t)p.total_tokens * p.heads;
+    const WinArgs a{p.lengths, p.tok_off, p.av_items, p.status, keys.first, keys.len, keys.rows, keys.max_len, q, k, v, out,
+                    ldq, ldk, ldv, ldo, p.heads, p.heads / kv_heads, window, sinks, scale, p.total_tokens, splits, ws,
+                    ws ? ws + (int64_t)splits * rows * kHeadDim : nullptr};
+    constexpr int64_t kUnit = 8 * kStreamRun;
+    const int64_t cap = std::max<int64_t>(p.av_cap, 1), limit = (int64_t)device_cu_count() * kWinPerCu;
+    const int64_t g = (std::min(cap, limit) + kUnit - 1) / kUnit * kUnit;
+    const dim3 grid((unsigned)g, (unsigned)splits);
+    if (dtype == 1) hipLaunchKernelGGL(k_attention_window<true>, grid, dim3(kWinThreads), 0, s, a);
+    else hipLaunchKernelGGL(k_attention_window<false>, grid, dim3(kWinThreads), 0, s, a);
+    if (splits > 1) {
+        const dim3 jg((unsigned)((rows + 3) / 4));
+        if (dtype == 1) hipLaunchKernelGGL(k_attention_window_join<true>, jg, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL(k_attention_window_join<false>, jg, dim3(256), 0, s, a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace rag

@@ -19,7 +19,7 @@ constexpr int kHeadDim = 64;  // head dimension the attention kernels are built 
 
 // Status-word bits (mirrors the public enum).
 constexpr int kDataNegLength = 1, kDataLongLength = 2, kDataTokenCount = 4, kDataQktCap = 8,
-              kDataAvCap = 16, kDataScoreCap = 32;
+              kDataAvCap = 16, kDataScoreCap = 32, kDataKvRange = 64;
 
 // Variable-sized batched GEMM: output tile, size limits and status-word bits
 // (mirror the public constants).

@@ -95,4 +95,18 @@ hipError_t launch_linear_i8(int dtype, const int8_t* x, int ldx, const float* x_
                             const float* w_scale, const void* bias, const void* residual, int ldr, int act, void* y,
                             int ldy, int T, int K, int N, hipStream_t s);
 
+// Sliding-window attention.  `first` and `len` NULL: each sequence's keys are its own tokens.
+struct WindowKeys {
+    const int64_t* first;
+    const int32_t* len;
+    int64_t rows;
+    int32_t max_len;
+};
+int window_splits(int64_t T, int64_t batch, int64_t heads, int64_t kv_heads, int64_t max_len, int64_t max_kv, int64_t window,
+                  int64_t sinks);
+size_t window_workspace(int64_t T, int64_t heads, int64_t splits);
+hipError_t launch_attention_window(const PlanView& p, int dtype, const void* q, int ldq, const void* k, int ldk,
+                                   const void* v, int ldv, const WindowKeys& keys, int kv_heads, float scale, int window,
+                                   int sinks, void* out, int ldo, int splits, void* workspace, hipStream_t s);
+
 }  // namespace rag

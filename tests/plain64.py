@@ -59,3 +59,42 @@ def rotary(x, pos, freq, amplitude, heads, head_dim, half, inverse=False):
     else:
         y[..., 0:2 * P:2], y[..., 1:2 * P:2] = z.real, z.imag
     return y.reshape(T, heads * head_dim)
+
+
+def window_attention(L, heads, kv_heads, q, k, v, first, kv_len, window, sinks, scale):
+    """Dense masked attention per sequence and head in float64.  Returns (out, magnitude, bound): magnitude is
+    sum_j p_j |v_j| of each output, bound the largest sum_c |q_c k_c| |scale| over a row's visible keys."""
+    T, G = q.shape[0], heads // kv_heads
+    q, k, v = q.double(), k.double(), v.double()
+    out, mag = torch.zeros(T, heads * 64, dtype=torch.float64), torch.zeros(T, heads * 64, dtype=torch.float64)
+    bound, count = torch.zeros(T, heads, dtype=torch.float64), torch.zeros(T, heads, dtype=torch.float64)
+    t0 = 0
+    for b, n in enumerate(L):
+        m = kv_len[b]
+        if n and m:
+            p = torch.arange(m - n, m)[:, None]
+            j = torch.arange(m)[None]
+            seen = (j <= p) & ((j > p - window) | (j < sinks))
+            for h in range(heads):
+                qq = q[t0:t0 + n, 64 * h:64 * h + 64]
+                g = 64 * (h // G)
+                kk, vv = k[first[b]:first[b] + m, g:g + 64], v[first[b]:first[b] + m, g:g + 64]
+                s = (qq @ kk.t() * scale).masked_fill(~seen, -math.inf)
+                e = torch.exp(s - s.amax(1, keepdim=True).clamp_min(-1e300))
+                e = e / e.sum(1, keepdim=True).clamp_min(1e-300)
+                out[t0:t0 + n, 64 * h:64 * h + 64] = e @ vv
+                mag[t0:t0 + n, 64 * h:64 * h + 64] = e @ vv.abs()
+                a = (qq.abs() @ kk.abs().t() * abs(scale)).masked_fill(~seen, 0.0)
+                bound[t0:t0 + n, h] = a.amax(1)
+                count[t0:t0 + n, h] = seen.sum(1)
+        t0 += n
+    return out, mag, bound, count
+
+
+def window_tolerance(dtype, ref, mag, bound, count):
+    """Half steps: a score is a sum of 64 products (64 roundings of at most `bound`), scaled (3); an
+    exponential then errs by that and 2; sums over the keys by one per key, in numerator and denominator, each
+    with a few of the rescalings; in bf16 every exponential of the product is rounded (2^-8), and the result is."""
+    each = 2 * 2.0 ** -24 * (67 * bound + count + 8)
+    each = each.repeat_interleave(64, dim=1)
+    return mag * (each + (HALF["bf16"] if dtype == "bf16" else 0.0)) + HALF[dtype] * ref.abs()

@@ -134,3 +134,67 @@ LINEAR_OK = dict(x=A, ldx=512, x_scale=A + MB, w=A + 2 * MB, w_scale=A + 3 * MB,
 def test_linear_i8_refuses(over, status):
     assert call("packed_linear_i8", LINEAR, LINEAR_OK, **over) == status
     assert call("packed_linear_i8", LINEAR, LINEAR_OK, T=0, x=None, w=None, y=None, x_scale=None, w_scale=None) == 0
+
+
+WINDOW = ("plan", "q", "ldq", "k", "ldk", "v", "ldv", "kv_heads", "head_dim", "scale", "window", "sinks", "out", "ldo", "ws",
+          "ws_bytes", "dtype", "stream")
+CACHED = WINDOW[:7] + ("kv_rows", "kv_first", "kv_len", "max_kv_len") + WINDOW[7:]
+
+
+def window_ok():
+    return dict(plan=plan(), q=A, ldq=512, k=A + MB, ldk=128, v=A + 2 * MB, ldv=128, kv_heads=2, head_dim=64, scale=0.125,
+                window=100, sinks=4, out=A + 3 * MB, ldo=512, ws=None, ws_bytes=0, dtype=BF16, stream=None, kv_rows=4096,
+                kv_first=A + 4 * MB, kv_len=A + 5 * MB, max_kv_len=128)
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(plan=None), ARG), (dict(dtype=9), DTYPE), (dict(kv_heads=0), SHAPE), (dict(kv_heads=3), SHAPE), (dict(kv_heads=16), SHAPE),
+    (dict(window=-1), ARG), (dict(sinks=-1), ARG), (dict(head_dim=128), SHAPE), (dict(scale=float("nan")), ARG),
+    (dict(q=None), ARG), (dict(k=None), ARG), (dict(v=None), ARG), (dict(out=None), ARG), (dict(ldq=504), SHAPE),
+    (dict(ldq=516), SHAPE), (dict(ldk=120), SHAPE), (dict(ldv=124), SHAPE), (dict(ldo=256), SHAPE), (dict(q=A + 8), SHAPE),
+    (dict(k=A + MB + 2), SHAPE), (dict(v=A + 2 * MB + 8), SHAPE), (dict(out=A + 3 * MB + 4), SHAPE), (dict(ldk=1 << 22), SHAPE),
+    (dict(ldo=1 << 22), SHAPE), (dict(out=A), ARG), (dict(out=A + MB), ARG), (dict(out=A + 2 * MB + 512), ARG),
+    (dict(dtype=F32, ldk=126 + 4), SHAPE), (dict(dtype=F32, q=A + 4), SHAPE)])
+def test_window_refuses(over, status):
+    ok = window_ok()
+    assert call("ragged_attention_window", WINDOW, ok, **over) == status
+    assert call("ragged_attention_window_cached", CACHED, ok, **over) == status
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(kv_rows=-1), ARG), (dict(kv_rows=1 << 41), ARG), (dict(kv_first=None), ARG), (dict(kv_len=None), ARG),
+    (dict(kv_first=A + 4 * MB + 4), ARG), (dict(kv_len=A + 5 * MB + 2), ARG), (dict(max_kv_len=-1), ARG),
+    (dict(out=A + 4 * MB, kv_first=A + 4 * MB + 1024), ARG), (dict(kv_len=A + 3 * MB + 4), ARG),
+    # one token of each of four sequences over long caches is split and needs its workspace
+    (dict(short=1, max_kv_len=100000, window=2 ** 31 - 1), WS), (dict(short=1, max_kv_len=100000, window=50000, ws=A + 6 * MB, ws_bytes=1000), WS),
+    (dict(short=1, max_kv_len=100000, window=50000, ws=None, ws_bytes=1 << 30), ARG),
+    (dict(short=1, max_kv_len=100000, window=50000, ws=A + 6 * MB + 8, ws_bytes=1 << 30), ARG),
+    (dict(short=1, max_kv_len=100000, window=50000, ws=A + 2 * MB, ws_bytes=1 << 30), ARG),
+    (dict(short=1, max_kv_len=100000, window=50000, ws=A + 3 * MB, ws_bytes=1 << 30), ARG)])
+def test_cached_window_refuses(over, status):
+    over = dict(over)
+    if over.pop("short", 0):
+        over["plan"] = plan(total_tokens=4, max_len=1)
+    assert call("ragged_attention_window_cached", CACHED, window_ok(), **over) == status
+
+
+def test_window_workspace():
+    f = lib().ragged_attention_window_workspace
+    n = ctypes.c_size_t()
+    assert f(plan(), 128, 2, 100, 4, BF16, ctypes.byref(n)) == 0
+    assert f(plan(total_tokens=4, max_len=1), 100000, 2, 50000, 4, BF16, ctypes.byref(n)) == 0 and n.value > 0
+    big = n.value
+    assert f(plan(total_tokens=4, max_len=1), 100000, 2, 64, 4, BF16, ctypes.byref(n)) == 0 and n.value < big
+    assert f(plan(total_tokens=0, max_len=0), 0, 2, 64, 4, F32, ctypes.byref(n)) == 0 and n.value == 0
+    assert f(plan(), 128, 2, 100, 4, BF16, None) == ARG
+    assert f(plan(), 128, 3, 100, 4, BF16, ctypes.byref(n)) == SHAPE
+    assert f(plan(), 128, 2, -1, 4, BF16, ctypes.byref(n)) == ARG
+    assert f(plan(), -1, 2, 1, 4, BF16, ctypes.byref(n)) == ARG
+    assert f(plan(total_tokens=2 ** 30, max_len=2 ** 12), 128, 2, 1, 4, BF16, ctypes.byref(n)) == SHAPE
+    assert f(plan(), 128, 2, 100, 4, 5, ctypes.byref(n)) == DTYPE
+
+
+def test_nothing_to_attend():
+    ok = dict(window_ok(), plan=plan(total_tokens=0, max_len=0), q=None, k=None, v=None, out=None)
+    assert call("ragged_attention_window", WINDOW, ok) == 0
+    assert call("ragged_attention_window_cached", CACHED, ok) == 0
