@@ -276,60 +276,83 @@ def packed_layernorm(x, gamma, beta, y, eps=1e-5, stream=None):
                                             _dtype_code(x), _stream(stream)))
 
 
-def _like(name, t, shape, dtype):
-    """`t` is None or a tensor of this shape and type."""
-    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
-        raise ValueError(f"{name} must be {list(shape)} of {dtype}, not {list(t.shape)} of {t.dtype}")
+# The operators below check types, shapes and devices of what they are given; a step of
+# single tokens takes as long as its host side, so the checks are one comparison each and
+# pointers go to ctypes as integers.
+
+def _refuse(name, t, shape, dtype, dev):
+    raise ValueError(f"{name} must be {list(shape)} of {dtype} on device {dev} with unit stride in its last dimension, "
+                     f"not {list(t.shape)} of {t.dtype} on {t.device}, strides {list(t.stride())}")
 
 
-def _vector(name, t, n, dtype):
-    """`t` is None or a contiguous vector of n elements."""
-    _like(name, t, (n,), dtype)
-    if t is not None and not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+def _mat(name, t, shape, dtype, dev):
+    """Leading dimension of a matrix of this shape (a tuple) and type; 0 for None."""
+    if t is None:
+        return 0
+    ld = t.stride()
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or ld[1] != 1:
+        _refuse(name, t, shape, dtype, dev)
+    return ld[0]
+
+
+def _vec(name, t, n, dtype, dev):
+    """Address of a contiguous vector of n elements; None for None."""
+    if t is None:
+        return None
+    if t.shape != (n,) or t.dtype is not dtype or t.get_device() != dev or (n > 1 and t.stride()[0] != 1):
+        _refuse(name, t, (n,), dtype, dev)
+    return t.data_ptr()
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _launch_stream(stream, dev):
+    """The stream to launch on: tensors of another device than the current one are refused."""
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError("the tensors must be on the current device")
+    # (the current stream's handle; building the Stream object takes longer than the call)
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def packed_rmsnorm(x, gamma, y=None, eps=1e-6, residual=None, x_out=None, q=None, q_scale=None, stream=None):
     """h = x + residual, and its RMS norm times gamma: into `y`, into the 8-bit rows `q` (int8)
     and `q_scale` (float32 [T]), or both; `x_out` receives h.  `y` and `x_out` may be x or residual."""
-    T, d = x.shape
-    for name, t in (("y", y), ("residual", residual), ("x_out", x_out)):
-        _like(name, t, x.shape, x.dtype)
-    _vector("gamma", gamma, d, x.dtype)
-    _like("q", q, x.shape, torch.int8)
-    _vector("q_scale", q_scale, T, torch.float32)
-    ld = [0 if t is None else _ld(t) for t in (residual, x_out, y, q)]
-    _check("packed_rmsnorm", _c_rmsnorm(_ptr(x), _ld(x), _ptr(residual), ld[0], _ptr(gamma), eps, _ptr(x_out), ld[1],
-                                        _ptr(y), ld[2], _ptr(q), ld[3], _ptr(q_scale), T, d, _dtype_code(x),
-                                        _stream(stream)))
+    shape, dt, dev = x.shape, x.dtype, x.get_device()
+    T, d = shape
+    st = _c_rmsnorm(x.data_ptr(), _mat("x", x, shape, dt, dev), _addr(residual), _mat("residual", residual, shape, dt, dev),
+                    _vec("gamma", gamma, d, dt, dev), eps, _addr(x_out), _mat("x_out", x_out, shape, dt, dev),
+                    _addr(y), _mat("y", y, shape, dt, dev), _addr(q), _mat("q", q, shape, torch.int8, dev),
+                    _vec("q_scale", q_scale, T, torch.float32, dev), T, d, _dtype_code(x), _launch_stream(stream, dev))
+    if st:
+        _check("packed_rmsnorm", st)
 
 
 def packed_quantize_i8(x, q, scale, stream=None):
     """8-bit rows of x [T, d] (tokens, or a weight matrix): q int8 [T, d], scale float32 [T]."""
-    T, d = x.shape
-    _like("q", q, x.shape, torch.int8)
-    _vector("scale", scale, T, torch.float32)
-    _check("packed_quantize_i8", _c_quantize_i8(_ptr(x), _ld(x), _ptr(q), _ld(q), _ptr(scale), T, d, _dtype_code(x),
-                                                _stream(stream)))
+    shape, dev = x.shape, x.get_device()
+    T, d = shape
+    st = _c_quantize_i8(x.data_ptr(), _mat("x", x, shape, x.dtype, dev), _addr(q), _mat("q", q, shape, torch.int8, dev),
+                        _vec("scale", scale, T, torch.float32, dev), T, d, _dtype_code(x), _launch_stream(stream, dev))
+    if st:
+        _check("packed_quantize_i8", st)
 
 
 def packed_linear_i8(x, x_scale, w, w_scale, y, bias=None, residual=None, act=RAG_ACT_NONE, stream=None):
     """y = act(x_scale w_scale (x w^T) + bias) + residual: x int8 [T, K] and w int8 [N, K] in 8-bit rows with
     their float32 scales ([T] and [N]); bias, residual and y (which may be residual) of one type."""
+    dt, dev = y.dtype, y.get_device()
     T, K = x.shape
     N = w.shape[0]
-    _like("x", x, (T, K), torch.int8)
-    _like("w", w, (N, K), torch.int8)
-    if not w.is_contiguous():
+    if _mat("w", w, (N, K), torch.int8, dev) != K and N > 1:
         raise ValueError("w must be contiguous")
-    _vector("x_scale", x_scale, T, torch.float32)
-    _vector("w_scale", w_scale, N, torch.float32)
-    _like("y", y, (T, N), y.dtype)
-    _vector("bias", bias, N, y.dtype)
-    _like("residual", residual, (T, N), y.dtype)
-    _check("packed_linear_i8", _c_linear_i8(_ptr(x), _ld(x), _ptr(x_scale), _ptr(w), _ptr(w_scale), _ptr(bias),
-                                            _ptr(residual), 0 if residual is None else _ld(residual), act, _ptr(y),
-                                            _ld(y), T, K, N, _dtype_code(y), _stream(stream)))
+    st = _c_linear_i8(x.data_ptr(), _mat("x", x, (T, K), torch.int8, dev), _vec("x_scale", x_scale, T, torch.float32, dev),
+                      w.data_ptr(), _vec("w_scale", w_scale, N, torch.float32, dev), _vec("bias", bias, N, dt, dev),
+                      _addr(residual), _mat("residual", residual, (T, N), dt, dev), act, y.data_ptr(),
+                      _mat("y", y, (T, N), dt, dev), T, K, N, _dtype_code(y), _launch_stream(stream, dev))
+    if st:
+        _check("packed_linear_i8", st)
 
 
 def rotary_frequencies(rot_dim, base=10000.0, scaling=RAG_ROTARY_PLAIN, factor=1.0, orig_len=0, beta_fast=32.0,
@@ -347,13 +370,14 @@ def packed_rotary(plan: Plan, x, y, inv_freq, heads, head_dim=RAG_HEAD_DIM, layo
     """Turns the first 2 * len(inv_freq) channels of each of `heads` heads of x [T, heads * head_dim] into y (which
     may be x).  inv_freq is a float64 device tensor; pos_start int32 [B] holds each sequence's first position;
     `inverse` turns back."""
-    _like("x", x, (plan.total_tokens, heads * head_dim), x.dtype)
-    _like("y", y, x.shape, x.dtype)
-    _vector("inv_freq", inv_freq, inv_freq.numel(), torch.float64)
-    _vector("pos_start", pos_start, plan.batch, torch.int32)
-    _check("packed_rotary", _c_rotary(plan.ref(), _ptr(x), _ld(x), _ptr(y), _ld(y), heads, head_dim,
-                                      2 * inv_freq.numel(), layout | (RAG_ROTARY_INVERSE if inverse else 0),
-                                      _ptr(inv_freq), amplitude, _ptr(pos_start), _dtype_code(x), _stream(stream)))
+    dt, dev, n = x.dtype, x.get_device(), inv_freq.numel()
+    shape = (plan.total_tokens, heads * head_dim)
+    st = _c_rotary(plan.ref(), x.data_ptr(), _mat("x", x, shape, dt, dev), y.data_ptr(), _mat("y", y, shape, dt, dev), heads,
+                   head_dim, 2 * n, layout | (RAG_ROTARY_INVERSE if inverse else 0),
+                   _vec("inv_freq", inv_freq, n, torch.float64, dev), amplitude,
+                   _vec("pos_start", pos_start, plan.batch, torch.int32, dev), _dtype_code(x), _launch_stream(stream, dev))
+    if st:
+        _check("packed_rotary", st)
 
 
 def ragged_attention_window_workspace(plan: Plan, max_kv_len, window, sinks=0, kv_heads=None, dtype=torch.bfloat16):
@@ -365,16 +389,16 @@ def ragged_attention_window_workspace(plan: Plan, max_kv_len, window, sinks=0, k
     return n.value
 
 
-def _window_operands(plan, q, k, v, out, kv_heads, head_dim, workspace):
-    _like("q", q, (plan.total_tokens, plan.heads * head_dim), q.dtype)
-    _like("out", out, q.shape, q.dtype)
-    _like("k", k, (k.shape[0], kv_heads * head_dim), q.dtype)
-    _like("v", v, k.shape, q.dtype)
+def _window_operands(plan, q, k, v, out, kv_rows, kv_heads, head_dim, workspace):
+    """(dtype code, device, leading dimensions of q, k, v and out, workspace address and bytes)"""
+    dt, dev = q.dtype, q.get_device()
+    shape, kv = (plan.total_tokens, plan.heads * head_dim), (kv_rows, kv_heads * head_dim)
+    lds = (_mat("q", q, shape, dt, dev), _mat("k", k, kv, dt, dev), _mat("v", v, kv, dt, dev), _mat("out", out, shape, dt, dev))
     if workspace is None:
-        return None, 0
-    if not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous")
-    return _ptr(workspace), workspace.numel() * workspace.element_size()
+        return _dtype_code(q), dev, lds, None, 0
+    if not workspace.is_contiguous() or workspace.get_device() != dev:
+        raise ValueError("workspace must be contiguous and on the operands' device")
+    return _dtype_code(q), dev, lds, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def ragged_attention_window(plan: Plan, q, k, v, out, scale, window, sinks=0, kv_heads=None, head_dim=RAG_HEAD_DIM,
@@ -382,24 +406,25 @@ def ragged_attention_window(plan: Plan, q, k, v, out, scale, window, sinks=0, kv
     """Causal attention over the packed batch: position p sees keys j <= p with j > p - window or j < sinks.
     k and v hold kv_heads (default: all) heads, each shared by plan.heads / kv_heads query heads."""
     kvh = kv_heads or plan.heads
-    ws, n = _window_operands(plan, q, k, v, out, kvh, head_dim, workspace)
-    _like("k", k, (plan.total_tokens, kvh * head_dim), q.dtype)
-    _check("ragged_attention_window", _c_window(plan.ref(), _ptr(q), _ld(q), _ptr(k), _ld(k), _ptr(v), _ld(v), kvh,
-                                                head_dim, scale, window, sinks, _ptr(out), _ld(out), ws, n,
-                                                _dtype_code(q), _stream(stream)))
+    code, dev, ld, ws, n = _window_operands(plan, q, k, v, out, plan.total_tokens, kvh, head_dim, workspace)
+    st = _c_window(plan.ref(), q.data_ptr(), ld[0], k.data_ptr(), ld[1], v.data_ptr(), ld[2], kvh, head_dim, scale, window,
+                   sinks, out.data_ptr(), ld[3], ws, n, code, _launch_stream(stream, dev))
+    if st:
+        _check("ragged_attention_window", st)
 
 
 def ragged_attention_window_cached(plan: Plan, q, k, v, kv_first, kv_len, max_kv_len, out, scale, window, sinks=0,
                                    kv_heads=None, head_dim=RAG_HEAD_DIM, workspace=None, stream=None):
     """The same over caches k and v [rows, kv_heads * head_dim]: sequence b's keys are the kv_len[b] rows from
     kv_first[b] (int32 and int64 device tensors), its queries the last plan.lengths[b] of those positions."""
-    kvh = kv_heads or plan.heads
-    ws, n = _window_operands(plan, q, k, v, out, kvh, head_dim, workspace)
-    _vector("kv_first", kv_first, plan.batch, torch.int64)
-    _vector("kv_len", kv_len, plan.batch, torch.int32)
-    _check("ragged_attention_window_cached", _c_window_cached(
-        plan.ref(), _ptr(q), _ld(q), _ptr(k), _ld(k), _ptr(v), _ld(v), k.shape[0], _ptr(kv_first), _ptr(kv_len), max_kv_len,
-        kvh, head_dim, scale, window, sinks, _ptr(out), _ld(out), ws, n, _dtype_code(q), _stream(stream)))
+    kvh, rows = kv_heads or plan.heads, k.shape[0]
+    code, dev, ld, ws, n = _window_operands(plan, q, k, v, out, rows, kvh, head_dim, workspace)
+    st = _c_window_cached(plan.ref(), q.data_ptr(), ld[0], k.data_ptr(), ld[1], v.data_ptr(), ld[2], rows,
+                          _vec("kv_first", kv_first, plan.batch, torch.int64, dev),
+                          _vec("kv_len", kv_len, plan.batch, torch.int32, dev), max_kv_len, kvh, head_dim, scale, window,
+                          sinks, out.data_ptr(), ld[3], ws, n, code, _launch_stream(stream, dev))
+    if st:
+        _check("ragged_attention_window_cached", st)
 
 
 def encoder_layer_workspace(total_tokens, max_len, d_model, heads, d_ff, dtype=RAG_BF16, flags=0):
