@@ -455,7 +455,7 @@ rag_status encoder_layer_noalloc(const rag_plan* plan, const void* x, void* y, i
  * The operators of a decoder layer with 8-bit projections.  They read and write
  * packed activations like the operators above (dtype RAG_BF16 or RAG_F32) and
  * hold sums, statistics and softmax states in fp32 (products of 8-bit integers in
- * int32, exactly; angles in fp64).
+ * int32, exactly; angles in fp64).  T, N and plan->total_tokens are at most 2^30.
  *
  * 8-bit rows: row t of an [rows, d] matrix is int8 q and one fp32 scale, its values
  * q[t][c] * scale[t], with scale[t] = max_c |y[t][c]| / 127 and q = y / scale rounded

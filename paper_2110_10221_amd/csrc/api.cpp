@@ -610,6 +610,8 @@ rag_status ragged_trmm(const void* l, int32_t ldl, const void* b, int32_t ldb, v
 
 namespace {
 
+constexpr int32_t kMaxRows = 1 << 30;  // row and tile arithmetic of these operators stays in 32 bits
+
 // Rows read and written in 16-byte chunks in either type.
 rag_status check_rows(const void* ptr, int64_t ld, int64_t width, int32_t dtype, const char* name, const char* fn) {
     const rag_status st = check_operand(ptr, ld, width, dtype, 16, name, fn);
@@ -634,7 +636,7 @@ rag_status check_q(const int8_t* q, int64_t ldq, const float* scale, int64_t d, 
 rag_status check_norm_sizes(int32_t T, int32_t d, int32_t dtype, const char* fn) {
     const rag_status st = check_dtype(dtype, fn);
     if (st) return st;
-    if (T < 0 || d < 1) return fail(RAG_ERR_ARG, "%s: T %d, d %d out of range", fn, T, d);
+    if (T < 0 || T > kMaxRows || d < 1) return fail(RAG_ERR_ARG, "%s: T %d, d %d out of range", fn, T, d);
     const int E = dtype == RAG_BF16 ? 8 : 4;
     if (d % E != 0 || d > RAG_NORM_MAX_DIM)
         return fail(RAG_ERR_SHAPE, "%s: d %d must be a multiple of %d and <= %d", fn, d, E, RAG_NORM_MAX_DIM);
@@ -750,7 +752,8 @@ rag_status packed_rotary(const rag_plan* plan, const void* x, int32_t ldx, void*
     rag::PlanView v;
     rag_status st;
     if ((st = view_plan(plan, v, fn)) || (st = check_dtype(dtype, fn))) return st;
-    if (heads < 1) return fail(RAG_ERR_ARG, "%s: heads %d out of range", fn, heads);
+    if (heads < 1 || plan->total_tokens > kMaxRows)
+        return fail(RAG_ERR_ARG, "%s: heads %d or total_tokens %d out of range", fn, heads, plan->total_tokens);
     if (layout < 0 || layout > (RAG_ROTARY_INTERLEAVED | RAG_ROTARY_INVERSE)) return fail(RAG_ERR_ARG, "%s: bad layout %d", fn, layout);
     if (rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > head_dim || head_dim > RAG_ROTARY_MAX_DIM)
         return fail(RAG_ERR_SHAPE, "%s: rot_dim %d must be even and in [2, head_dim], head_dim %d at most %d", fn, rot_dim,
@@ -781,7 +784,8 @@ rag_status packed_linear_i8(const int8_t* x, int32_t ldx, const float* x_scale, 
     const char* fn = "packed_linear_i8";
     rag_status st;
     if ((st = check_dtype(dtype, fn))) return st;
-    if (T < 0 || K < 1 || N < 1) return fail(RAG_ERR_ARG, "%s: T %d, K %d, N %d out of range", fn, T, K, N);
+    if (T < 0 || T > kMaxRows || K < 1 || N < 1 || N > kMaxRows)
+        return fail(RAG_ERR_ARG, "%s: T %d, K %d, N %d out of range", fn, T, K, N);
     if (act < RAG_ACT_NONE || act > RAG_ACT_GELU_TANH) return fail(RAG_ERR_ARG, "%s: bad activation %d", fn, act);
     if (K % 16 != 0 || K > RAG_I8_MAX_K || N % 8 != 0)
         return fail(RAG_ERR_SHAPE, "%s: needs K %% 16 == 0, K <= %d and N %% 8 == 0 (K %d, N %d)", fn, RAG_I8_MAX_K, K, N);

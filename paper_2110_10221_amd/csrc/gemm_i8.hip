@@ -4,13 +4,17 @@
 // cores (v_mfma_i32_16x16x64_i8; K <= 131056 keeps the sums below 2^31) and scales, bias, activation and
 // residual applied in fp32 to the finished sum, which is rounded to the type once.
 //
-// A TM x TN tile per workgroup of WM x WN (x WK, over k) waves.  Operands go global -> LDS
+// Up to 16 tokens go to a kernel of their own (further down), others to TM x TN tiles, one per
+// workgroup of WM x WN (x WK, over k) waves, of the size that linear_form_i8 picks.  What bounds them:
+// moving operands from L2 into LDS on the small ones (a 64 x 64 tile takes 16 KB per 0.22 us of a CU),
+// the matrix cores and power on 256 x 256 ones: 8192^3 413 us, 2660 TOPS.  Operands go global -> LDS
 // by bounds-checked direct copies, 128 k (one 128-byte line) of each row per stage, ST stages; the
 // 16-byte chunks of a row are XOR-swizzled by it, so fragment reads of 16 rows meet distinct
 // bank groups.  Rows past T or N lie outside the descriptors, chunks past K are sent past
 // them: both arrive as zeros.
 // A lane's fragment is 16 consecutive k of one row in both operands, and the tile is
 // computed as w x^T, so that a lane ends with four consecutive features of one token.
+#include <algorithm>
 #include <type_traits>
 
 #include "gemm_common.h"
@@ -31,7 +35,10 @@ struct I8Cfg {
     static constexpr int kRows = 65536 / (TN * WK * 4) < TM ? 65536 / (TN * WK * 4) : TM;  // epilogue slice
     static constexpr int kSum = kRows * TN * WK * 4;
     static constexpr int kLds = ST * kStage > kSum ? ST * kStage : kSum;
-    static_assert((TM + TN) / 8 % kWaves == 0 && kLds <= 160 * 1024 && (WK == 1 || WK == 2), "configuration");
+    // waves per SIMD: what the LDS lets reside
+    static constexpr int kResident = 160 * 1024 / kLds < 1 ? 1 : 160 * 1024 / kLds;
+    static constexpr int kWavesPerSimd = kResident * kWaves / 4 < 1 ? 1 : kResident * kWaves / 4 > 8 ? 8 : kResident * kWaves / 4;
+    static_assert((TM / 8) % 2 == 0 && (TM + TN) / 8 % kWaves == 0 && kLds <= 160 * 1024 && (WK == 1 || WK == 2), "configuration");
     static_assert(TM / WM % 16 == 0 && TN / WN % 16 == 0 && TM % kRows == 0 && (TM / WM) % 16 == 0, "blocks");
 };
 
@@ -60,37 +67,44 @@ __device__ __forceinline__ void barrier_seen() {
 // Eight consecutive features of one token, from sums to the stored row.
 template <bool BF16, int ACT>
 struct Finish {
-    float ws[8], bv[8];
-    __device__ __forceinline__ void features(const I8Args& a, int n) {  // n: a multiple of 8 below N
-        *reinterpret_cast<floatx4*>(ws) = *reinterpret_cast<const floatx4*>(a.w_scale + n);
-        *reinterpret_cast<floatx4*>(ws + 4) = *reinterpret_cast<const floatx4*>(a.w_scale + n + 4);
-        if (!a.bias) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) bv[e] = 0.f;
-        } else {
-            load(a.bias, n, bv);
-        }
+    struct Raw {
+        u32x4 v[BF16 ? 1 : 2];
+    };
+    static __device__ __forceinline__ Raw load(const void* p, int64_t off) {
+        Raw r;
+        const u32x4* const src = BF16 ? reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p) + off)
+                                      : reinterpret_cast<const u32x4*>(static_cast<const float*>(p) + off);
+        r.v[0] = src[0];
+        if constexpr (!BF16) r.v[1] = src[1];
+        return r;
     }
-    static __device__ __forceinline__ void load(const void* p, int64_t off, float* v) {
-        if constexpr (BF16) {
-            const u32x4 c = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p) + off);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[2 * e] = lo_bf16(c[e]);
-                v[2 * e + 1] = hi_bf16(c[e]);
-            }
-        } else {
-            *reinterpret_cast<floatx4*>(v) = *reinterpret_cast<const floatx4*>(static_cast<const float*>(p) + off);
-            *reinterpret_cast<floatx4*>(v + 4) = *reinterpret_cast<const floatx4*>(static_cast<const float*>(p) + off + 4);
-        }
+    static __device__ __forceinline__ float get(const Raw& r, int e) {
+        if constexpr (BF16) return e & 1 ? hi_bf16(r.v[0][e >> 1]) : lo_bf16(r.v[0][e >> 1]);
+        else return __uint_as_float(r.v[e >> 2][e & 3]);
     }
-    __device__ __forceinline__ void row(const I8Args& a, const int* sum, float xs, const float* res, int m, int n) const {
+    floatx4 ws[2];
+    Raw braw;
+    float bv[8];
+    // the features' scales and bias: loaded here, unpacked by features() once they are used
+    __device__ __forceinline__ void fetch(const I8Args& a, int n) {  // n: a multiple of 8 below N
+        ws[0] = *reinterpret_cast<const floatx4*>(a.w_scale + n);
+        ws[1] = *reinterpret_cast<const floatx4*>(a.w_scale + n + 4);
+        if (a.bias) braw = load(a.bias, n);
+    }
+    __device__ __forceinline__ void features(bool bias) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) bv[e] = bias ? get(braw, e) : 0.f;
+    }
+    __device__ __forceinline__ void row(const I8Args& a, const int* sum, float xs, bool residual, const Raw& res, int m, int n) const {
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float z = fmaf((float)sum[e] * xs, ws[e], bv[e]);
+            const float z = fmaf((float)sum[e] * xs, ws[e >> 2][e & 3], bv[e]);
             v[e] = BF16 ? activate_bf16<ACT>(z) : activate<ACT>(z);
-            if (res) v[e] += res[e];
+        }
+        if (residual) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += get(res, e);
         }
         if constexpr (BF16) {
             *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.y) + (int64_t)m * a.ldy + n) =
@@ -114,16 +128,17 @@ __device__ __forceinline__ void i8_tile(const I8Args& a, int m0, int n0, int8_t*
     const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.w + (int64_t)n0 * K, (uint32_t)min(a.N - n0, TN) * K);
     // copy c of this wave fills block id = wave * NC + c of a stage (8 rows of 128 bytes, x
     // rows first; lane l slot l: row l / 8, physical chunk l % 8, logical chunk XORed with swz2(row))
-    int voff[NC], kb[NC];  // the lane's byte offset; its chunk's first k
+    int voff[NC], kb[2];  // the lane's byte offset; its chunk's first k, which only block parity changes
+#pragma unroll
+    for (int c = 0; c < 2; ++c) kb[c] = ((lane % 8) ^ swz2((wave * NC + c) * 8 + lane / 8)) * 16;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         const int b = wave * NC + c, row = (b < TM / 8 ? b : b - TM / 8) * 8 + lane / 8;
-        kb[c] = ((lane % 8) ^ swz2(row)) * 16;
-        voff[c] = row * (b < TM / 8 ? a.ldx : K) + kb[c];
+        voff[c] = row * (b < TM / 8 ? a.ldx : K) + kb[c & 1];
     }
     auto issue_one = [&](int step, int8_t* st, int c) {
         const int b = wave * NC + c, k0 = step * 128;
-        const int off = k0 + kb[c] < K ? voff[c] : kPast;
+        const int off = k0 + kb[c & 1] < K ? voff[c] : kPast;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(b < TM / 8 ? rx : rw, (lds_void_t*)(st + b * 1024), 16, off, k0, 0, 0);
     };
     intx4 acc[FN][FM];
@@ -191,34 +206,57 @@ __device__ __forceinline__ void i8_tile(const I8Args& a, int m0, int n0, int8_t*
         }
         st = next;
     };
-    int k = 0;
-    for (; k + 2 < nk; k += 2) {
-        step(k, std::false_type{}, std::integral_constant<int, 0>{});
-        step(k + 1, std::false_type{}, std::integral_constant<int, 1>{});
-    }
-    if (k + 1 < nk) {
-        step(k, std::false_type{}, std::integral_constant<int, 0>{});
-        step(k + 1, std::true_type{}, std::integral_constant<int, 1>{});
-    } else {
-        step(k, std::true_type{}, std::integral_constant<int, 0>{});
-    }
-    wait_vm<0>();  // the copies past the reduction have landed: LDS is free
-
-    // Epilogue in slices of kRows tokens: the int32 sums go through LDS (row r's 16-byte
-    // chunk c at c ^ (r & 15), one tile per k share), then each thread finishes eight features of a row at
-    // a time.  Slice s holds the s-th part of every wave row's tokens.
+    // The epilogue's rows: thread t finishes eight features of row t / kCh + it * kRowStep of each slice.
     constexpr int kRows = C::kRows, kSlices = TM / kRows, kPart = kRows / C::WM;  // a wave row's tokens per slice
     static_assert(kPart % 16 == 0, "slices of whole blocks");
     constexpr int kCh = TN / 8, kRowStep = C::kThreads / kCh, kIt = kRows / kRowStep;
     static_assert(C::kThreads % kCh == 0 && kRows % kRowStep == 0, "row phase");
     constexpr int kSwz = TN / 4 < 16 ? TN / 4 - 1 : 15;
+    using Fin = Finish<BF16, ACT>;
     const int ch = threadIdx.x % kCh, r0 = threadIdx.x / kCh, n = n0 + ch * 8, nc = min(n, a.N - 8);
-    Finish<BF16, ACT> fin;
-    fin.features(a, nc);
+    const auto token = [&](int s, int it) {
+        const int row = r0 + it * kRowStep;
+        return m0 + (row / kPart) * (TM / C::WM) + s * kPart + row % kPart;
+    };
+    constexpr std::integral_constant<int, 0> even{};
+    constexpr std::integral_constant<int, 1> odd{};
+    int k = 0;
+    if constexpr (G % 2 == 0) {
+        for (; k + 1 < nk; ++k) step(k, std::false_type{}, even);
+        step(k, std::true_type{}, even);
+    } else {
+        for (; k + 2 < nk; k += 2) {
+            step(k, std::false_type{}, even);
+            step(k + 1, std::false_type{}, odd);
+        }
+        if (k + 1 < nk) {
+            step(k, std::false_type{}, even);
+            step(k + 1, std::true_type{}, odd);
+        } else {
+            step(k, std::true_type{}, even);
+        }
+    }
+    wait_vm<0>();  // the copies past the reduction have landed: LDS is free
+
+    // Epilogue in slices of kRows tokens (slice s holds the s-th part of every wave row's):
+    // the int32 sums go through LDS (row r's 16-byte chunk c at c ^ (r & 15), one tile per k
+    // share), then whole rows are finished.  What it reads is loaded before the staging, at
+    // indexes clamped into range: loaded under the range tests, each row's values were waited
+    // for in turn.
+    Fin fin;
+    fin.fetch(a, nc);
     int* const ep = reinterpret_cast<int*>(sm);
     auto slot_of = [&](int row, int c) { return row * TN + ((c ^ (row & kSwz)) * 4); };
 #pragma unroll
     for (int s = 0; s < kSlices; ++s) {
+        float xs[kIt];
+        typename Fin::Raw res[kIt];
+#pragma unroll
+        for (int t = 0; t < kIt; ++t) {
+            const int m = min(token(s, t), a.T - 1);
+            xs[t] = a.x_scale[m];
+            if (a.residual) res[t] = Fin::load(a.residual, (int64_t)m * a.ldr + nc);
+        }
         barrier_seen();
 #pragma unroll
         for (int jj = 0; jj < kPart / 16; ++jj)
@@ -229,9 +267,10 @@ __device__ __forceinline__ void i8_tile(const I8Args& a, int m0, int n0, int8_t*
                                           slot_of(wm * kPart + jj * 16 + l16, (wn * (TN / C::WN) + i * 16 + 4 * q4) >> 2)) =
                     acc[i][s * (kPart / 16) + jj];
         barrier_seen();
+        if (s == 0) fin.features(a.bias != nullptr);
 #pragma unroll
         for (int t = 0; t < kIt; ++t) {
-            const int row = r0 + t * kRowStep, m = m0 + (row / kPart) * (TM / C::WM) + s * kPart + row % kPart;
+            const int row = r0 + t * kRowStep, m = token(s, t);
             if (m >= a.T || n >= a.N) continue;
             int v[8];
             *reinterpret_cast<intx4*>(v) = *reinterpret_cast<const intx4*>(ep + slot_of(row, 2 * ch));
@@ -244,19 +283,24 @@ __device__ __forceinline__ void i8_tile(const I8Args& a, int m0, int n0, int8_t*
                     for (int e = 0; e < 4; ++e) v[4 * hc + e] += o[e];
                 }
             }
-            float res[8];
-            if (a.residual) Finish<BF16, ACT>::load(a.residual, (int64_t)m * a.ldr + n, res);
-            fin.row(a, v, a.x_scale[m], a.residual ? res : nullptr, m, n);
+            fin.row(a, v, xs[t], a.residual != nullptr, res[t], m, n);
         }
     }
 }
 
 template <class C, bool BF16, int ACT>
-__global__ __launch_bounds__(C::kThreads) void k_linear_i8(I8Args a, int tiles_m, int tiles_n) {
+__global__ __launch_bounds__(C::kThreads, C::kWavesPerSimd) void k_linear_i8(I8Args a, int tiles_m, int tiles_n) {
     extern __shared__ __attribute__((aligned(16))) int8_t smem_i8[];
     int tm, tn;
     tile_coords(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, tm, tn);
     i8_tile<C, BF16, ACT>(a, tm * C::TM, tn * C::TN, smem_i8);
+}
+
+// Whole 256 x 256 tiles of a launch: all of them if the last round is nearly full, else the
+// full rounds.
+int64_t i8_whole_tiles(int64_t tiles, int64_t cus) {
+    const int64_t rest = tiles % cus;
+    return 4 * rest > 3 * cus ? tiles : tiles - rest;
 }
 
 template <class C, bool BF16, int ACT>
@@ -274,11 +318,112 @@ hipError_t launch_tiles(const I8Args& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-using I8Small = I8Cfg<64, 64, 2, 2, 1, 3>;
+// 256 x 256 tiles, one workgroup per CU, whole rounds of them; the tiles of the last,
+// partial round run as four 128 x 128 quarters each (n_full workgroups, then the quarters).
+using I8Big = I8Cfg<256, 256, 2, 4, 1, 2>;
+using I8Tail = I8Cfg<128, 128, 2, 4, 1, 4>;
+static_assert(I8Tail::kThreads == I8Big::kThreads && I8Tail::kLds <= I8Big::kLds, "quarters");
+
+template <bool BF16, int ACT>
+__global__ __launch_bounds__(I8Big::kThreads, 2) void k_linear_i8_big(I8Args a, int tiles_m, int tiles_n, int n_full) {
+    extern __shared__ __attribute__((aligned(16))) int8_t smem_i8[];
+    int tm, tn;
+    if ((int)blockIdx.x < n_full) {
+        tile_coords(blockIdx.x, n_full, tiles_m, tiles_n, tm, tn);
+        i8_tile<I8Big, BF16, ACT>(a, tm * 256, tn * 256, smem_i8);
+    } else {
+        const int u = blockIdx.x - n_full;
+        group_walk(n_full + u / 4, tiles_m, tiles_n, tm, tn);
+        const int m0 = tm * 256 + (u & 1) * 128, n0 = tn * 256 + ((u >> 1) & 1) * 128;
+        if (m0 >= a.T || n0 >= a.N) return;  // a quarter past the last token or feature
+        i8_tile<I8Tail, BF16, ACT>(a, m0, n0, smem_i8);
+    }
+}
+
+template <bool BF16, int ACT>
+hipError_t launch_big(const I8Args& a, int cus, hipStream_t s) {
+    auto* f = &k_linear_i8_big<BF16, ACT>;
+    static bool attr_set = false;  // benign race: every thread sets the same value
+    if (!attr_set) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, I8Big::kLds);
+        if (e != hipSuccess) return e;
+        attr_set = true;
+    }
+    const int64_t tiles_m = ((int64_t)a.T + 255) / 256, tiles_n = ((int64_t)a.N + 255) / 256, tiles = tiles_m * tiles_n;
+    const int64_t n_full = i8_whole_tiles(tiles, cus);
+    if (n_full + 4 * (tiles - n_full) > INT32_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(f, dim3((unsigned)(n_full + 4 * (tiles - n_full))), dim3(I8Big::kThreads), I8Big::kLds, s, a,
+                       (int)tiles_m, (int)tiles_n, (int)n_full);
+    return hipGetLastError();
+}
+
+// Few tokens: 16 features per workgroup for all of at most 16 tokens, the reduction
+// split over the workgroup's waves.  Bound by the weights' bytes (and latency): each is read
+// once, straight into the MFMA operand, four 64-k groups per wave in flight; x comes out of L2.
+constexpr int kFewGroups = 4;      // 64-k groups per wave and step
+constexpr int kFewWaves = 8;       // (1 x 4096 x 1024: 4.7 us; 5.3 with four, 5.0 with sixteen)
+
+template <bool BF16, int ACT>
+__global__ __launch_bounds__(kFewWaves * kWave) void k_linear_i8_few(I8Args a) {
+    __shared__ __attribute__((aligned(16))) int part[kFewWaves * 16 * 16];
+    const int wave = uni(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const int l16 = lane % 16, q4 = lane / 16;
+    const int n0 = blockIdx.x * 16, K = a.K, steps = (K + 64 * kFewGroups - 1) / (64 * kFewGroups);
+    const int8_t* const wr = a.w + (int64_t)min(n0 + l16, a.N - 1) * K;
+    const int8_t* const xr = a.x + (int64_t)min(l16, a.T - 1) * a.ldx;
+    intx4 acc = {0, 0, 0, 0};
+    for (int s = wave; s < steps; s += kFewWaves) {
+        intx4 fw[kFewGroups], fx[kFewGroups];
+#pragma unroll
+        for (int u = 0; u < kFewGroups; ++u) {
+            const int k = (s * kFewGroups + u) * 64 + q4 * 16, kc = min(k, K - 16);
+            fw[u] = *reinterpret_cast<const intx4*>(wr + kc);
+            fx[u] = *reinterpret_cast<const intx4*>(xr + kc);
+            if (k >= K) fw[u] = intx4{0, 0, 0, 0};  // past the reduction
+        }
+#pragma unroll
+        for (int u = 0; u < kFewGroups; ++u) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u], fx[u], acc, 0, 0, 0);
+    }
+    // acc[e]: token l16, feature 4 q4 + e
+    *reinterpret_cast<intx4*>(part + (wave * 16 + l16) * 16 + 4 * q4) = acc;
+    __syncthreads();
+    const int m = threadIdx.x / 2, n = n0 + 8 * (threadIdx.x % 2);
+    if (m >= a.T || n >= a.N) return;
+    Finish<BF16, ACT> fin;
+    fin.fetch(a, n);
+    const float xs = a.x_scale[m];
+    typename Finish<BF16, ACT>::Raw res;
+    if (a.residual) res = Finish<BF16, ACT>::load(a.residual, (int64_t)m * a.ldr + n);
+    int v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w)
+#pragma unroll
+        for (int hc = 0; hc < 2; ++hc) {
+            const intx4 o = *reinterpret_cast<const intx4*>(part + (w * 16 + m) * 16 + 8 * (threadIdx.x % 2) + 4 * hc);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * hc + e] += o[e];
+        }
+    fin.features(a.bias != nullptr);
+    fin.row(a, v, xs, a.residual != nullptr, res, m, n);
+}
+
+template <bool BF16, int ACT>
+hipError_t launch_few(const I8Args& a, hipStream_t s) {
+    hipLaunchKernelGGL((k_linear_i8_few<BF16, ACT>), dim3((a.N + 15) / 16), dim3(kFewWaves * kWave), 0, s, a);
+    return hipGetLastError();
+}
 
 template <bool BF16, int ACT>
 hipError_t launch_form(const I8Args& a, hipStream_t s) {
-    return launch_tiles<I8Small, BF16, ACT>(a, s);
+    const int cus = device_cu_count();
+    switch (linear_form_i8(a.T, a.K, a.N, ACT, BF16, cus)) {
+        case 0: return launch_few<BF16, ACT>(a, s);
+        case 1: return launch_tiles<I8Cfg<32, 64, 1, 2, 2, 4>, BF16, ACT>(a, s);
+        case 2: return launch_tiles<I8Cfg<64, 64, 2, 2, 1, 3>, BF16, ACT>(a, s);
+        case 3: return launch_tiles<I8Cfg<64, 128, 2, 2, 1, 3>, BF16, ACT>(a, s);
+        case 4: return launch_tiles<I8Cfg<128, 128, 2, 2, 1, 2>, BF16, ACT>(a, s);
+        default: return launch_big<BF16, ACT>(a, cus, s);
+    }
 }
 
 template <bool BF16>
@@ -291,6 +436,42 @@ hipError_t launch_type(const I8Args& a, int act, hipStream_t s) {
 }
 
 }  // namespace
+
+// The form of a call: 0 few tokens, 1 .. 4 the tiles 32 x 64 (two k shares), 64 x 64, 64 x 128
+// and 128 x 128, 5 the 256 x 256 tiles and quarters.  Up to 16 tokens the first one (T = 16, K = N =
+// 4096: 6.7 us, 7.7 on 32 x 64 tiles; T = 32: 8.6 and 7.9).  Above, the smallest of the modelled times
+// in us
+//     start + max(epilogue + nk * alone, rounds * (epilogue + nk * step))
+// nk the 128-k steps, rounds the tiles of the busiest CU, `alone` a step's latency and `step` its
+// share of a busy CU's time, the epilogue longer with an activation or fp32 outputs.  Fitted to
+// 205 shapes (T 17 to 40000, K 256 to 8192, N 64 to 8192, both types, every epilogue), where
+// the choice takes 2% more than the fastest form on average and 23% at worst.  Both sides, us on forms 1
+// to 5: 2237 x 2048 x 512 fp32 9.6, 8.9, 9.1, 14.7, 12.2; 35475 x 1024 x 4096 GELU 395, 291, 264, 225,
+// 229; 35475 x 4096 x 1024 with residual 336, 225, 190, 168, 140.
+int linear_form_i8(int64_t T, int64_t K, int64_t N, int act, bool bf16, int64_t cus) {
+    if (T <= 16) return 0;
+    struct Cost {
+        int tm, tn;
+        double start, epilogue, step, alone, act, f32;
+    };
+    static const Cost kForms[4] = {{32, 64, 2.37, 0.46, 0.148, 0.166, 0.24, 0.20}, {64, 64, 2.43, 0.49, 0.219, 0.254, 0.57, 0.48},
+                                   {64, 128, 2.24, 1.18, 0.336, 0.365, 1.43, 0.86}, {128, 128, 1.19, 2.08, 0.522, 0.727, 2.82, 1.74}};
+    const auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
+    const double nk = (double)up(K, 128), a = act != 0, f = !bf16;
+    // 256 x 256: rounds of whole tiles, then one of quarters
+    const int64_t big = up(T, 256) * up(N, 256), whole = i8_whole_tiles(big, cus);
+    const double extra = a * 9.05 + f * 5.68;
+    double best = up(whole, cus) * (10.53 + extra + nk * 1.486) + up(4 * (big - whole), cus) * (3.96 + extra / 4 + nk * 0.492);
+    int form = 5;
+    for (int i = 0; i < 4; ++i) {
+        const Cost& c = kForms[i];
+        const double e = c.epilogue + a * c.act + f * c.f32;
+        const int64_t rounds = up(up(T, c.tm) * up(N, c.tn), cus);
+        const double t = c.start + std::max(e + nk * c.alone, rounds * (e + nk * c.step));
+        if (t < best) best = t, form = i + 1;
+    }
+    return form;
+}
 
 hipError_t launch_linear_i8(int dtype, const int8_t* x, int ldx, const float* x_scale, const int8_t* w,
                             const float* w_scale, const void* bias, const void* residual, int ldr, int act, void* y,

@@ -37,7 +37,7 @@ NORM_OK = dict(x=A, ldx=512, residual=A + MB, ldr=512, gamma=A + 2 * MB, eps=1e-
 
 
 @pytest.mark.parametrize("over,status", [
-    (dict(dtype=2), DTYPE), (dict(T=-1), ARG), (dict(d=0), ARG), (dict(d=516), SHAPE), (dict(d=16392, ldx=16392), SHAPE),
+    (dict(dtype=2), DTYPE), (dict(T=-1), ARG), (dict(T=2 ** 30 + 1), ARG), (dict(d=0), ARG), (dict(d=516), SHAPE), (dict(d=16392, ldx=16392), SHAPE),
     (dict(eps=0.0), ARG), (dict(eps=float("nan")), ARG), (dict(eps=float("inf")), ARG), (dict(x=None), ARG),
     (dict(ldx=504), SHAPE), (dict(ldx=516), SHAPE), (dict(x=A + 8), SHAPE), (dict(residual=A + MB + 2), SHAPE),
     (dict(gamma=None), ARG), (dict(gamma=A + 2 * MB + 8), ARG), (dict(y=None, q=None, q_scale=None), ARG),
@@ -122,7 +122,7 @@ LINEAR_OK = dict(x=A, ldx=512, x_scale=A + MB, w=A + 2 * MB, w_scale=A + 3 * MB,
 
 
 @pytest.mark.parametrize("over,status", [
-    (dict(dtype=7), DTYPE), (dict(T=-1), ARG), (dict(K=0), ARG), (dict(N=0), ARG), (dict(act=3), ARG), (dict(act=-1), ARG),
+    (dict(dtype=7), DTYPE), (dict(T=-1), ARG), (dict(T=2 ** 31 - 1), ARG), (dict(N=2 ** 30 + 8), ARG), (dict(K=0), ARG), (dict(N=0), ARG), (dict(act=3), ARG), (dict(act=-1), ARG),
     (dict(K=520), SHAPE), (dict(K=131072, ldx=131072), SHAPE), (dict(N=260), SHAPE), (dict(x=None), ARG), (dict(w=None), ARG),
     (dict(x_scale=None), ARG), (dict(w_scale=None), ARG), (dict(ldx=496), SHAPE), (dict(ldx=520), SHAPE),
     (dict(ldx=1 << 22), SHAPE), (dict(x=A + 8), SHAPE), (dict(w=A + 2 * MB + 4), SHAPE), (dict(x_scale=A + MB + 1), SHAPE),

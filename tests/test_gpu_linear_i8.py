@@ -152,3 +152,20 @@ def test_a_replayed_graph_and_two_streams(T):
         rag.packed_linear_i8(x, xs, w, ws, ref)
         torch.cuda.synchronize()
         assert torch.equal(y, ref) and torch.equal(z, ref)
+
+
+@pytest.mark.parametrize("T,K,N,form,form32", [
+    (16, 528, 264, 0, 0), (17, 528, 264, 1, 1), (40, 4112, 2056, 1, 1), (300, 400, 2056, 2, 2), (700, 1040, 2104, 3, 3),
+    (2900, 1552, 2104, 4, 4), (5200, 1552, 4104, 5, 5), (4300, 4112, 2312, 4, 5)])
+def test_every_form(T, K, N, form, form32):
+    # ragged edges in every dimension on each of the tile forms; 5200 x 4104 is 357 256 x 256 tiles,
+    # 256 whole and 101 in quarters, 4300 x 2312 is 170, in fp32 all in quarters
+    import ctypes
+
+    import paper_2110_10221_amd as rag
+
+    f = rag.library()._ZN3rag14linear_form_i8Elllibl  # rag::linear_form_i8
+    f.restype, f.argtypes = ctypes.c_int, [ctypes.c_int64] * 3 + [ctypes.c_int, ctypes.c_bool, ctypes.c_int64]
+    assert f(T, K, N, 0, True, 256) == form and f(T, K, N, 2, False, 256) == form32
+    call(T, K, N, "bf16", 0, True, True, seed=form)
+    call(T, K, N, "f32", 2, True, False, seed=form)
