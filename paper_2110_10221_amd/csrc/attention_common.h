@@ -6,9 +6,6 @@
 
 namespace rag {
 
-typedef __attribute__((ext_vector_type(4))) short short4_t;
-typedef __attribute__((address_space(3))) short4_t lds_short4_t;
-
 __device__ __forceinline__ u32x4 ld16(const uint16_t* p) { return *reinterpret_cast<const u32x4*>(p); }
 
 // Element offset of (row, col) in [rows][64 channels] LDS storage (128-byte rows,

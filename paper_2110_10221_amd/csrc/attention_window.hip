@@ -52,6 +52,8 @@ struct WinArgs {
     int window, sinks;
     float scale;
     int T, splits;
+    int stride;      // between the list entries that hold rows: G where no sequence has more than one tile a key head
+    int dealt;       // entries go to the XCDs in runs (else one by one)
     float* part_o;   // [splits][T][heads][64] unnormalised outputs
     float* part_ml;  // [splits][T][heads][2] reference and sum
 };
@@ -74,12 +76,6 @@ struct WinT<false> {
 // The last key before position p's window (keys above it are in the window), at least -1.
 __device__ __forceinline__ int window_below(int p, int window) {
     return (int)max((int64_t)p - window, (int64_t)-1);
-}
-
-// ds_read_b64_tr_b16: within 16 lanes, lane 4 e + q addresses row e, columns 4 q .. 4 q + 3 of a
-// 4 x 16 block and receives column (lane % 16) of its rows.
-__device__ __forceinline__ u32x2 read_tr(const uint16_t* p) {
-    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)p));
 }
 
 __device__ __forceinline__ floatx16 mfma32x32x2(float a, float b, const floatx16& c) {
@@ -107,27 +103,38 @@ void k_attention_window(WinArgs a) {
     constexpr int kEs = (int)sizeof(T);
     if (a.status[0] != 0) return;
     __shared__ __attribute__((aligned(16))) uint8_t kvs[2 * kStage];
-    const int n_items = uni(a.status[2]);
+    const int n_items = uni(a.status[2]) / a.stride;
     const int wave = uni(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int l32 = lane % 32, h2 = lane / 32;
     // (a zero scale would turn hidden keys' -inf into NaN; below 1e-30 every exponential is 1 anyway)
     const float zs = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-30f);
     const bool flip = a.scale < 0.f;
     const int G = a.group;
+    // LDS addresses of the transposed V reads in stage 0, key step 0: within 16 lanes, lane 4 e + q
+    // addresses row e, columns 4 q .. 4 q + 3 of a 4 x 16 block and receives column (lane % 16)
+    uint32_t vaddr[2][2];
+#pragma unroll
+    for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi)
+            vaddr[cb][hi] = (uint32_t)(uintptr_t)(lds_void_t*)kvs +
+                            2 * kv_off(4 * (lane / 32) + (lane % 16) / 4 + 8 * hi, 32 * cb + 16 * (lane / 16 % 2) + 4 * (lane % 4));
 
     for (int base = 0; base < n_items; base += gridDim.x) {
-        const int it = base + stream_item(blockIdx.x, gridDim.x);
+        const int it = base + (a.dealt ? stream_item(blockIdx.x, gridDim.x) : (int)blockIdx.x);
         if (it >= n_items) break;
-        const int b = uni(a.av_items[3 * it]), h = uni(a.av_items[3 * it + 1]), ti = uni(a.av_items[3 * it + 2]);
-        const int L = uni(a.lengths[b]), t0 = uni(a.tok_off[b]);
+        const int32_t* const entry = a.av_items + 3 * (int64_t)it * a.stride;
+        // (each line's loads go out together: an item's start is a chain of three)
+        const int b = uni(entry[0]), h = uni(entry[1]), ti = uni(entry[2]);
+        const int len = a.lengths[b], off = a.tok_off[b], kvn = a.kv_len ? a.kv_len[b] : len;
+        const int64_t kv0 = a.kv_len ? a.kv_first[b] : off;
+        const int L = uni(len), t0 = uni(off);
         const int hk = h / G, rows = L * G;
         const int r0 = ((h - hk * G) * ((L + kTile - 1) / kTile) + ti) * kTile;
         if (r0 >= rows) continue;
-        int n = L;  // keys
-        int64_t first = t0;
+        const int n = uni(kvn);  // keys
+        const int64_t first = uni64(kv0);
         if (a.kv_len) {
-            n = uni(a.kv_len[b]);
-            first = uni64(a.kv_first[b]);
             if (n < 0 || n > a.max_kv || first < 0 || first > a.kv_rows - n) {
                 if (threadIdx.x == 0) atomicOr(a.status, kDataKvRange);
                 continue;
@@ -138,7 +145,9 @@ void k_attention_window(WinArgs a) {
         const int w0 = r0 + wave * 32;
         const bool active = w0 < rows;
         const int row = min(w0 + l32, rows - 1), tok = row / G, head = hk * G + (row - tok * G);
-        const int p = past + tok, below = window_below(p, a.window);
+        // a row sees the `range` keys from `from` on, and the sinks up to its position p
+        const int p = past + tok, from = window_below(p, a.window) + 1;
+        const uint32_t range = (uint32_t)max(p + 1 - from, 0);
         const int plo = past + min(w0, rows - 1) / G, phi = past + min(w0 + 31, rows - 1) / G;
         const int tlo = past + r0 / G, thi = past + min(r0 + kTile - 1, rows - 1) / G;
         // chunks: window [cw0, cw1) downwards, then the sinks' [0, cs) below them
@@ -150,6 +159,12 @@ void k_attention_window(WinArgs a) {
         const int per = (nch + a.splits - 1) / a.splits;
         const int i0 = min(nch, (int)blockIdx.y * per), i1 = min(nch, i0 + per);
         const auto chunk = [&](int i) { return i < nwin ? cw1 - 1 - i : cs - 1 - (i - nwin); };
+        // of the wave's rows: the last chunk that any sees (-1: none) and the first of the windows; chunks
+        // [whole0, whole1) are seen whole by all, and those below sinks0 that end before whole1;
+        // chunks from sinks1 on hold no sink
+        const int last = active && phi >= 0 ? phi / kWinChunk : -1, wfirst = (window_below(plo, a.window) + 1) / kWinChunk;
+        const int whole0 = (window_below(phi, a.window) + kWinChunk) / kWinChunk, whole1 = plo >= 0 ? (plo + 1) / kWinChunk : 0;
+        const int sinks0 = a.sinks / kWinChunk, sinks1 = a.sinks / kWinChunk + (a.sinks % kWinChunk != 0);
 
         // copy i of this wave fills rows 1 KB apart from block wave * kBlocks + i of K and V;
         // rows past the last key arrive as zeros.  The descriptor starts at the chunk, so a
@@ -162,12 +177,13 @@ void k_attention_window(WinArgs a) {
             vko[i] = r * a.ldk * kEs + c;
             vvo[i] = r * a.ldv * kEs + c;
         }
+        const T* const kbase = static_cast<const T*>(a.k) + first * a.ldk + hk * kHeadDim;
+        const T* const vbase = static_cast<const T*>(a.v) + first * a.ldv + hk * kHeadDim;
+        const int tail_chunk = n / kWinChunk, tail = n % kWinChunk;  // the chunk that the last key cuts
         const auto issue = [&](int i, auto stg) {
-            const int k0 = chunk(i) * kWinChunk, valid = min(kWinChunk, n - k0);
-            const __amdgpu_buffer_rsrc_t rk = chunk_rsrc(
-                static_cast<const T*>(a.k) + (first + k0) * a.ldk + hk * kHeadDim, (uint32_t)valid * a.ldk * kEs);
-            const __amdgpu_buffer_rsrc_t rv = chunk_rsrc(
-                static_cast<const T*>(a.v) + (first + k0) * a.ldv + hk * kHeadDim, (uint32_t)valid * a.ldv * kEs);
+            const int c = chunk(i), valid = c == tail_chunk ? tail : kWinChunk;
+            const __amdgpu_buffer_rsrc_t rk = chunk_rsrc(kbase + (int64_t)c * (kWinChunk * a.ldk), (uint32_t)(valid * a.ldk) * kEs);
+            const __amdgpu_buffer_rsrc_t rv = chunk_rsrc(vbase + (int64_t)c * (kWinChunk * a.ldv), (uint32_t)(valid * a.ldv) * kEs);
             uint8_t* const st = kvs + decltype(stg)::value * kStage;
 #pragma unroll
             for (int i2 = 0; i2 < kBlocks; ++i2) {
@@ -200,23 +216,25 @@ void k_attention_window(WinArgs a) {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's copies of chunk i
             attn_barrier();  // ... and the other wave's; the other stage was last read in step i - 1
             if (i + 1 < i1) issue(i + 1, std::integral_constant<int, 1 - STG>{});
-            const int c0 = chunk(i) * kWinChunk, c1 = c0 + kWinChunk - 1;
-            if (!active || c0 > phi || (c1 <= window_below(plo, a.window) && c0 >= a.sinks)) return;
-            // every key visible to every row?
-            const bool whole = c1 <= plo && (c0 > window_below(phi, a.window) || c1 < a.sinks);
+            const int c = chunk(i), c0 = c * kWinChunk;
+            if (c > last || (c < wfirst && c >= sinks1)) return;  // no row of the wave sees a key of it
+            const bool whole = c < whole1 && (c >= whole0 || c < sinks0);
             const uint8_t* const kst = kvs + STG * kStage;
             const uint8_t* const vst = kst + kWinChunk * W::kRow;
-            const auto visible = [&](int j) { return j <= p && (j > below || j < a.sinks); };
+            const auto visible = [&](int j) { return ((uint32_t)(j - from) < range) | ((j < a.sinks) & (j <= p)); };
             floatx16 acc;
-            const auto scores = [&] {
+            // (LEAN: a K fragment at a time, for the rare recomputation, where V is already held)
+            const auto products = [&](auto lean) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[r] = 0.f;
                 if constexpr (BF16) {
                     const uint16_t* const ks = reinterpret_cast<const uint16_t*>(kst);
+                    u32x4 kf[4];
 #pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        acc = mfma32x32x16(as_bf16x8(*reinterpret_cast<const u32x4*>(ks + kv_off(l32, 16 * u + 8 * h2))),
-                                           as_bf16x8(qf[u]), acc);
+                    for (int u = 0; u < 4; ++u) kf[u] = *reinterpret_cast<const u32x4*>(ks + kv_off(l32, 16 * u + 8 * h2));
+                    if constexpr (!decltype(lean)::value) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) acc = mfma32x32x16(as_bf16x8(kf[u]), as_bf16x8(qf[u]), acc);
                 } else {
 #pragma unroll
                     for (int u = 0; u < 8; ++u) {
@@ -226,10 +244,19 @@ void k_attention_window(WinArgs a) {
                         for (int e = 0; e < 4; ++e) acc = mfma32x32x2(kf[e], q4[e], acc);
                     }
                 }
+            };
+            const auto hide = [&] {
                 if (!whole) {
+                    if (c >= sinks1) {
+                        const int j0 = c0 + 4 * h2 - from;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (!visible(c0 + 8 * (r / 4) + 4 * h2 + (r % 4))) acc[r] = -INFINITY;
+                        for (int r = 0; r < 16; ++r)
+                            acc[r] = (uint32_t)(j0 + 8 * (r / 4) + (r % 4)) < range ? acc[r] : -INFINITY;
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            acc[r] = visible(c0 + 4 * h2 + 8 * (r / 4) + (r % 4)) ? acc[r] : -INFINITY;
+                    }
                 }
             };
             const auto chunk_max = [&] {
@@ -248,13 +275,38 @@ void k_attention_window(WinArgs a) {
                 for (int r = 0; r < 4; ++r) s[r] += s[r + 4];
                 return (s[0] + s[2]) + (s[1] + s[3]);
             };
-            scores();
+            products(std::false_type{});
+            // V^T operand: the lane's keys 16 t + {4 h2 .. + 3, 8 + 4 h2 .. + 3} of channel 32 cb + l32, by transposed
+            // reads whose latency passes under the products above (inline assembly, its own wait
+            // included: at the builtin the compiler waits for every copy into LDS, the next chunk's
+            // too)
+            u32x2 tr[2][2][2];
+            if constexpr (BF16) {
+                __builtin_amdgcn_sched_barrier(0);
+                asm volatile(
+                    "ds_read_b64_tr_b16 %0, %8 offset:%12\n\t"
+                    "ds_read_b64_tr_b16 %1, %9 offset:%12\n\t"
+                    "ds_read_b64_tr_b16 %2, %10 offset:%12\n\t"
+                    "ds_read_b64_tr_b16 %3, %11 offset:%12\n\t"
+                    "ds_read_b64_tr_b16 %4, %8 offset:%13\n\t"
+                    "ds_read_b64_tr_b16 %5, %9 offset:%13\n\t"
+                    "ds_read_b64_tr_b16 %6, %10 offset:%13\n\t"
+                    "ds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
+                    "s_waitcnt lgkmcnt(0)"
+                    : "=&v"(tr[0][0][0]), "=&v"(tr[0][0][1]), "=&v"(tr[0][1][0]), "=&v"(tr[0][1][1]),
+                      "=&v"(tr[1][0][0]), "=&v"(tr[1][0][1]), "=&v"(tr[1][1][0]), "=&v"(tr[1][1][1])
+                    : "v"(vaddr[0][0]), "v"(vaddr[0][1]), "v"(vaddr[1][0]), "v"(vaddr[1][1]),
+                      "i"(STG * kStage + kWinChunk * W::kRow), "i"(STG * kStage + kWinChunk * W::kRow + 16 * W::kRow)
+                    : "memory");
+            }
+            hide();
             if (fresh) m = fmaxf(chunk_max(), -FLT_MAX);  // (no visible key: any later score is far above)
             float ps = exps();
             // a lane sum above kSumCap (or NaN) means a score well above m: raise m to the
             // chunk's maximum and rescale what has been summed
             if (!fresh && __ballot(!(ps <= kSumCap)) != 0) {
-                scores();
+                products(std::true_type{});
+                hide();
                 const float mn = fmaxf(m, chunk_max());
                 const float alpha = __builtin_amdgcn_exp2f(m - mn);
                 lsum *= alpha;
@@ -283,16 +335,6 @@ void k_attention_window(WinArgs a) {
             };
             if constexpr (BF16) {
                 const uint16_t* const vs = reinterpret_cast<const uint16_t*>(vst);
-                // transposed reads: lane's keys 16 t + {4 h2 .. + 3, 8 + 4 h2 .. + 3} of channel 32 cb + l32
-                const int e4 = (lane % 16) / 4, q4 = lane % 4, g4 = lane / 16;
-                u32x2 tr[2][2][2];
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int cb = 0; cb < 2; ++cb)
-#pragma unroll
-                        for (int hi = 0; hi < 2; ++hi)
-                            tr[t][cb][hi] = read_tr(vs + 16 * t * kHeadDim + kv_off(4 * (g4 >> 1) + e4 + 8 * hi, 32 * cb + 16 * (g4 & 1) + 4 * q4));
                 if (!whole) {
                     bool bad = false;
 #pragma unroll
@@ -401,43 +443,83 @@ void k_attention_window(WinArgs a) {
     }
 }
 
-// Joins the splits' states of one (token, head) row per wave, a channel per lane.
+// Joins the splits' states of one (token, head) row per workgroup: sixteen lanes of four channels
+// each take every sixteenth split, all their loads in flight at once.
+constexpr int kWinMaxSplits = 256, kJoinGroups = 16;
+
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_attention_window_join(WinArgs a) {
     if (a.status[0] != 0) return;
     using T = typename WinT<BF16>::T;
-    const int64_t rows = (int64_t)a.T * a.heads, r = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
-    const int lane = threadIdx.x % kWave;
-    if (r >= rows) return;
-    float m = -FLT_MAX;
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[2 * (s * rows + r)]);
-    float sum = 0.f, o = 0.f;
-    for (int s = 0; s < a.splits; ++s) {
-        const float w = __builtin_amdgcn_exp2f(a.part_ml[2 * (s * rows + r)] - m);
-        sum = fmaf(w, a.part_ml[2 * (s * rows + r) + 1], sum);
-        o = fmaf(w, a.part_o[(s * rows + r) * kHeadDim + lane], o);
+    constexpr int kPer = kWinMaxSplits / kJoinGroups;
+    __shared__ float wmax[4], wsum[4];
+    __shared__ __attribute__((aligned(16))) float wout[4][kHeadDim];
+    const int64_t rows = (int64_t)a.T * a.heads, r = blockIdx.x;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, g = threadIdx.x / 16, c = lane % 16 * 4;
+    float ms[kPer], ls[kPer], m = -FLT_MAX;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f}, os[kPer];
+    const int n = (a.splits - g + kJoinGroups - 1) / kJoinGroups;  // this group's splits (may be none)
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        if (i * kJoinGroups >= a.splits) break;
+        const int64_t slot = (int64_t)min(g + i * kJoinGroups, a.splits - 1) * rows + r;
+        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * slot);
+        os[i] = *reinterpret_cast<const floatx4*>(a.part_o + slot * kHeadDim + c);
+        ms[i] = ml.x;
+        ls[i] = ml.y;
+        m = fmaxf(m, ml.x);
     }
-    o *= 1.0f / sum;
+    m = wave_max(m);
+    if (lane == 0) wmax[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(wmax[0], wmax[1]), fmaxf(wmax[2], wmax[3]));
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        if (i >= n) break;
+        const float w = __builtin_amdgcn_exp2f(ms[i] - m);
+        sum = fmaf(w, ls[i], sum);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(w, os[i][e], o[e]);
+    }
+    // the wave's four groups, then the four waves
+#pragma unroll
+    for (int d = 16; d <= 32; d *= 2) {
+        sum += __shfl_xor(sum, d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], d);
+    }
+    if (lane < 16) *reinterpret_cast<floatx4*>(&wout[wave][c]) = o;
+    if (lane == 0) wsum[wave] = sum;
+    __syncthreads();
+    if (threadIdx.x >= kHeadDim) return;
+    const float v = (wout[0][lane] + wout[1][lane] + wout[2][lane] + wout[3][lane]) / (wsum[0] + wsum[1] + wsum[2] + wsum[3]);
     T* const dst = static_cast<T*>(a.out) + (r / a.heads) * a.ldo + (r % a.heads) * kHeadDim + lane;
-    if constexpr (BF16) *dst = f32_to_bf16(o);
-    else *dst = o;
+    if constexpr (BF16) *dst = f32_to_bf16(v);
+    else *dst = v;
 }
 
 }  // namespace
 
-// Workgroups over the keys of one item: as many as fill the GPU where the batch has few
-// items, each with at least kWinSplitChunks chunks of the longest row.  (Whole GPUs' 256 CUs: the
-// workspace is sized by the same rule, on the host.)
+// Workgroups over the keys of one item: where the batch has few tiles, as many as bring four
+// workgroups to each CU, each with two chunks at least and no more of them than pays for the join: a chunk
+// takes about 0.6 us, the second launch 3 us and 0.07 us a split.  Up to eight chunks that never pays, above
+// the time is least at sqrt(8 chunks) splits.
+// One sequence of 1000 tokens, window 512, 16/4 heads: 13.4 us on two splits, 10.6 on four, 10.1
+// on eight; of 32768 tokens, 8 heads: 18.8 us on 68, 22.1 on 128; 32 sequences, window 4096, 16/4 heads:
+// 32.7 us on eight, 35.8 on 16.  (A whole GPU's 256 CUs: the workspace is sized by the same rule, on the host.)
 int window_splits(int64_t T, int64_t batch, int64_t heads, int64_t kv_heads, int64_t max_len, int64_t max_kv, int64_t window,
                   int64_t sinks) {
-    constexpr int64_t kWinSplitChunks = 8, kWant = 256 * 4;
     if (T <= 0) return 1;
     const int64_t group = heads / kv_heads;
     // tiles of 64 rows that hold any; keys a tile walks: its rows' positions and window, or all
     const int64_t tiles = kv_heads * std::min((T * group + 63 * batch) / 64, batch * ((max_len * group + 63) / 64));
     const int64_t keys = std::min(max_kv, std::min(window, max_kv) + std::min(sinks, max_kv) + std::min<int64_t>(max_len, 64));
-    const int64_t chunks = (keys + 31) / 32;
-    return (int)std::max<int64_t>(1, std::min({kWant / std::max<int64_t>(tiles, 1), chunks / kWinSplitChunks, (int64_t)256}));
+    const int64_t chunks = (keys + kWinChunk - 1) / kWinChunk;
+    const int64_t most = std::min({256 * 4 / std::max<int64_t>(tiles, 1), chunks / 2, (int64_t)kWinMaxSplits});
+    int64_t splits = 1;
+    while (chunks > 8 && splits < most && (splits + 1) * (splits + 1) <= 8 * chunks) ++splits;
+    return (int)splits;
 }
 
 size_t window_workspace(int64_t T, int64_t heads, int64_t splits) {
@@ -450,17 +532,24 @@ hipError_t launch_attention_window(const PlanView& p, int dtype, const void* q, 
     if (p.total_tokens == 0) return hipSuccess;
     float* const ws = static_cast<float*>(workspace);
     const int64_t rows = (int64_t)p.total_tokens * p.heads;
+    // Where every sequence's rows of a key head fill one tile (a step of single tokens), only
+    // the first of each G entries holds any, and only those are launched.  Neighbouring tiles
+    // of a prompt share keys and go to one XCD in runs; tiles of single tokens and splits share none and go
+    // to the XCDs in turn (in runs, eight heads' splits would all be one XCD's).
+    const int group = p.heads / kv_heads;
+    const bool single = (int64_t)p.max_len * group <= kTile;
+    const int stride = single ? group : 1, dealt = !single && splits == 1;
     const WinArgs a{p.lengths, p.tok_off, p.av_items, p.status, keys.first, keys.len, keys.rows, keys.max_len, q, k, v, out,
-                    ldq, ldk, ldv, ldo, p.heads, p.heads / kv_heads, window, sinks, scale, p.total_tokens, splits, ws,
+                    ldq, ldk, ldv, ldo, p.heads, group, window, sinks, scale, p.total_tokens, splits, stride, dealt, ws,
                     ws ? ws + (int64_t)splits * rows * kHeadDim : nullptr};
     constexpr int64_t kUnit = 8 * kStreamRun;
-    const int64_t cap = std::max<int64_t>(p.av_cap, 1), limit = (int64_t)device_cu_count() * kWinPerCu;
-    const int64_t g = (std::min(cap, limit) + kUnit - 1) / kUnit * kUnit;
+    const int64_t cap = std::max<int64_t>(p.av_cap / stride, 1), limit = (int64_t)device_cu_count() * kWinPerCu;
+    const int64_t g = dealt ? (std::min(cap, limit) + kUnit - 1) / kUnit * kUnit : std::min(cap, limit);
     const dim3 grid((unsigned)g, (unsigned)splits);
     if (dtype == 1) hipLaunchKernelGGL(k_attention_window<true>, grid, dim3(kWinThreads), 0, s, a);
     else hipLaunchKernelGGL(k_attention_window<false>, grid, dim3(kWinThreads), 0, s, a);
     if (splits > 1) {
-        const dim3 jg((unsigned)((rows + 3) / 4));
+        const dim3 jg((unsigned)rows);
         if (dtype == 1) hipLaunchKernelGGL(k_attention_window_join<true>, jg, dim3(256), 0, s, a);
         else hipLaunchKernelGGL(k_attention_window_join<false>, jg, dim3(256), 0, s, a);
     }
