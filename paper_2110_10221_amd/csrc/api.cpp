@@ -819,6 +819,7 @@ rag_status check_window(const rag_plan* plan, rag::PlanView& v, int32_t max_kv_l
     if ((st = view_plan(plan, v, fn)) || (st = check_dtype(dtype, fn))) return st;
     if (kv_heads < 1 || plan->heads % kv_heads != 0)
         return fail(RAG_ERR_SHAPE, "%s: %d heads are not a multiple of %d key heads", fn, plan->heads, kv_heads);
+    if (plan->heads > 32768) return fail(RAG_ERR_SHAPE, "%s: more than 32768 heads", fn);
     if (window < 0 || sinks < 0 || max_kv_len < 0)
         return fail(RAG_ERR_ARG, "%s: window %d, sinks %d, max_kv_len %d out of range", fn, window, sinks, max_kv_len);
     if (((int64_t)plan->total_tokens + RAG_TILE) * (plan->heads / kv_heads) > INT32_MAX)

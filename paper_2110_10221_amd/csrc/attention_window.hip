@@ -32,14 +32,15 @@
 namespace rag {
 namespace {
 
-constexpr int kWinWaves = 2, kWinThreads = kWinWaves * kWave;
+constexpr int kWinBlock = 32;       // rows per wave
+constexpr int kWinWaves = kTile / kWinBlock, kWinThreads = kWinWaves * kWave;
 constexpr int kWinChunk = 32;       // keys per LDS stage
-constexpr int kWinPerCu = 64;       // grid cap in workgroups per CU
 
 struct WinArgs {
     const int32_t* lengths;
     const int32_t* tok_off;
     const int32_t* av_items;
+    int64_t av_cap;
     int32_t* status;
     const int64_t* kv_first;  // NULL: the packed batch's own rows
     const int32_t* kv_len;
@@ -49,6 +50,7 @@ struct WinArgs {
     void* out;
     int ldq, ldk, ldv, ldo;
     int heads, group;  // query heads; query heads per key head
+    uint32_t magic;    // 2^32 / group, rounded up (0 for a group of one)
     int window, sinks;
     float scale;
     int T, splits;
@@ -73,6 +75,12 @@ struct WinT<false> {
     static __device__ __forceinline__ int swz(int row) { return row & 15; }
 };
 
+// Entry of a workgroup where neighbours go to one XCD in runs of kStreamRun.
+__device__ __forceinline__ int64_t dealt_item(int64_t bid) {
+    const int64_t xcd = bid % 8, j = bid / 8;
+    return ((j / kStreamRun) * 8 + xcd) * kStreamRun + j % kStreamRun;
+}
+
 // The last key before position p's window (keys above it are in the window), at least -1.
 __device__ __forceinline__ int window_below(int p, int window) {
     return (int)max((int64_t)p - window, (int64_t)-1);
@@ -93,7 +101,7 @@ __device__ __forceinline__ void copy_1k(__amdgpu_buffer_rsrc_t r, void* dst, int
 __device__ __forceinline__ bool finite_f32(float v) { return fabsf(v) <= FLT_MAX; }
 
 template <bool BF16>
-__global__ __launch_bounds__(kWinThreads, BF16 ? 4 : 2)
+__global__ __launch_bounds__(kWinThreads, BF16 ? 3 : 2)
 void k_attention_window(WinArgs a) {
     using W = WinT<BF16>;
     using T = typename W::T;
@@ -101,9 +109,7 @@ void k_attention_window(WinArgs a) {
     constexpr int kBlockRows = 1024 / W::kRow;             // rows of a 1 KB copy
     constexpr int kBlocks = kWinChunk / kBlockRows / kWinWaves;  // copies of K (and of V) per wave and chunk
     constexpr int kEs = (int)sizeof(T);
-    if (a.status[0] != 0) return;
-    __shared__ __attribute__((aligned(16))) uint8_t kvs[2 * kStage];
-    const int n_items = uni(a.status[2]) / a.stride;
+    __shared__ __attribute__((aligned(2 * kStage))) uint8_t kvs[2 * kStage];  // (stages a power of two apart: addresses toggle)
     const int wave = uni(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int l32 = lane % 32, h2 = lane / 32;
     // (a zero scale would turn hidden keys' -inf into NaN; below 1e-30 every exponential is 1 anyway)
@@ -120,383 +126,407 @@ void k_attention_window(WinArgs a) {
             vaddr[cb][hi] = (uint32_t)(uintptr_t)(lds_void_t*)kvs +
                             2 * kv_off(4 * (lane / 32) + (lane % 16) / 4 + 8 * hi, 32 * cb + 16 * (lane / 16 % 2) + 4 * (lane % 4));
 
-    for (int base = 0; base < n_items; base += gridDim.x) {
-        const int it = base + (a.dealt ? stream_item(blockIdx.x, gridDim.x) : (int)blockIdx.x);
-        if (it >= n_items) break;
-        const int32_t* const entry = a.av_items + 3 * (int64_t)it * a.stride;
-        // (each line's loads go out together: an item's start is a chain of three)
-        const int b = uni(entry[0]), h = uni(entry[1]), ti = uni(entry[2]);
-        const int len = a.lengths[b], off = a.tok_off[b], kvn = a.kv_len ? a.kv_len[b] : len;
-        const int64_t kv0 = a.kv_len ? a.kv_first[b] : off;
-        const int L = uni(len), t0 = uni(off);
-        const int hk = h / G, rows = L * G;
-        const int r0 = ((h - hk * G) * ((L + kTile - 1) / kTile) + ti) * kTile;
-        if (r0 >= rows) continue;
-        const int n = uni(kvn);  // keys
-        const int64_t first = uni64(kv0);
-        if (a.kv_len) {
-            if (n < 0 || n > a.max_kv || first < 0 || first > a.kv_rows - n) {
-                if (threadIdx.x == 0) atomicOr(a.status, kDataKvRange);
-                continue;
-            }
+    const int64_t bid = (int64_t)blockIdx.z * gridDim.x + blockIdx.x;
+    const int64_t it = (a.dealt ? dealt_item(bid) : bid) * a.stride;
+    // (each group's loads go out together: an item's start is a chain of three)
+    const int32_t* const entry = a.av_items + 3 * min(it, a.av_cap - 1);
+    const int errors = a.status[0], n_items = a.status[2], eb = entry[0], eh = entry[1], eti = entry[2];
+    if (uni(errors) != 0 || it >= uni(n_items)) return;
+    const int b = uni(eb), h = uni(eh), ti = uni(eti);
+    const int len = a.lengths[b], off = a.tok_off[b], kvn = a.kv_len ? a.kv_len[b] : len;
+    const int64_t kv0 = a.kv_len ? a.kv_first[b] : off;
+    const int L = uni(len), t0 = uni(off);
+    const auto per_group = [&](int x) { return G == 1 ? x : (int)__umulhi((uint32_t)x, a.magic); };  // x / G, x < 2^16
+    const int hk = uni(per_group(h)), rows = L * G;
+    const int r0 = ((h - hk * G) * ((L + kTile - 1) / kTile) + ti) * kTile;
+    if (r0 >= rows) return;
+    const int n = uni(kvn);  // keys
+    const int64_t first = uni64(kv0);
+    if (a.kv_len) {
+        if (n < 0 || n > a.max_kv || first < 0 || first > a.kv_rows - n) {
+            if (threadIdx.x == 0) atomicOr(a.status, kDataKvRange);
+            return;
         }
-        const int past = n - L;  // position of token 0
-        // the wave's rows and positions, and the tile's
-        const int w0 = r0 + wave * 32;
-        const bool active = w0 < rows;
-        const int row = min(w0 + l32, rows - 1), tok = row / G, head = hk * G + (row - tok * G);
-        // a row sees the `range` keys from `from` on, and the sinks up to its position p
-        const int p = past + tok, from = window_below(p, a.window) + 1;
-        const uint32_t range = (uint32_t)max(p + 1 - from, 0);
-        const int plo = past + min(w0, rows - 1) / G, phi = past + min(w0 + 31, rows - 1) / G;
-        const int tlo = past + r0 / G, thi = past + min(r0 + kTile - 1, rows - 1) / G;
-        // chunks: window [cw0, cw1) downwards, then the sinks' [0, cs) below them
-        int cw0 = (window_below(tlo, a.window) + 1) / kWinChunk, cw1 = thi / kWinChunk + 1;
-        if (thi < 0 || a.window == 0) cw0 = cw1 = INT32_MAX / kWinChunk;
-        const int seen_sinks = min(a.sinks, thi + 1);
-        const int cs = seen_sinks > 0 ? min((seen_sinks + kWinChunk - 1) / kWinChunk, cw0) : 0;
-        const int nwin = cw1 - cw0, nch = nwin + cs;
-        const int per = (nch + a.splits - 1) / a.splits;
-        const int i0 = min(nch, (int)blockIdx.y * per), i1 = min(nch, i0 + per);
-        const auto chunk = [&](int i) { return i < nwin ? cw1 - 1 - i : cs - 1 - (i - nwin); };
-        // of the wave's rows: the last chunk that any sees (-1: none) and the first of the windows; chunks
-        // [whole0, whole1) are seen whole by all, and those below sinks0 that end before whole1;
-        // chunks from sinks1 on hold no sink
-        const int last = active && phi >= 0 ? phi / kWinChunk : -1, wfirst = (window_below(plo, a.window) + 1) / kWinChunk;
-        const int whole0 = (window_below(phi, a.window) + kWinChunk) / kWinChunk, whole1 = plo >= 0 ? (plo + 1) / kWinChunk : 0;
-        const int sinks0 = a.sinks / kWinChunk, sinks1 = a.sinks / kWinChunk + (a.sinks % kWinChunk != 0);
+    }
+    const int past = n - L;  // position of token 0
+    // the tile's positions
+    const int tok0 = uni(G == 1 ? r0 : r0 / G), rem = r0 - tok0 * G;  // the tile's first row
+    const auto token = [&](int row) { return min(tok0 + per_group(rem + row), L - 1); };  // of a row of the tile
+    const int tlo = past + tok0, thi = past + uni(token(kTile - 1));
+    // chunks: window [cw0, cw1) downwards, then the sinks' [0, cs) below them
+    int cw0 = (window_below(tlo, a.window) + 1) / kWinChunk, cw1 = thi / kWinChunk + 1;
+    if (thi < 0 || a.window == 0) cw0 = cw1 = INT32_MAX / kWinChunk;
+    const int seen_sinks = min(a.sinks, thi + 1);
+    const int cs = seen_sinks > 0 ? min((seen_sinks + kWinChunk - 1) / kWinChunk, cw0) : 0;
+    const int nwin = cw1 - cw0, nch = nwin + cs;
+    const int per = (nch + a.splits - 1) / a.splits;
+    const int i0 = min(nch, (int)blockIdx.y * per), i1 = min(nch, i0 + per);
+    const auto chunk = [&](int i) { return i < nwin ? cw1 - 1 - i : cs - 1 - (i - nwin); };
+    const int sinks1 = a.sinks / kWinChunk + (a.sinks % kWinChunk != 0);  // chunks from here on hold no sink
+    // A row at position p sees the `range` keys from `from` on and those below sink_range.  Of the wave's rows: the
+    // last chunk that any sees (-1: none) and the first of the windows; chunks [whole0, whole1)
+    // are seen whole by all.
+    const int w0 = wave * kWinBlock, row = min(w0 + l32, rows - 1 - r0);
+    const bool active = r0 + w0 < rows;
+    const int tok = token(row), head = hk * G + (rem + row - (tok - tok0) * G);
+    const int p = past + tok, from = window_below(p, a.window) + 1;
+    const uint32_t range = (uint32_t)max(p + 1 - from, 0);
+    const int sink_range = min(a.sinks, p + 1);
+    const int plo = past + uni(token(w0)), phi = past + uni(token(w0 + kWinBlock - 1));
+    const int last = active && phi >= 0 ? phi / kWinChunk : -1, wfrom = window_below(plo, a.window) + 1, wfirst = wfrom / kWinChunk;
+    const int whole0 = (window_below(phi, a.window) + kWinChunk) / kWinChunk, whole1 = plo >= 0 ? (plo + 1) / kWinChunk : 0;
 
-        // copy i of this wave fills rows 1 KB apart from block wave * kBlocks + i of K and V;
-        // rows past the last key arrive as zeros.  The descriptor starts at the chunk, so a
-        // cache of any size is in reach.
-        int vko[kBlocks], vvo[kBlocks];
+    // copy i of this wave fills rows 1 KB apart from block wave * kBlocks + i of K and V;
+    // rows past the last key arrive as zeros.  The descriptor starts at the chunk, so a
+    // cache of any size is in reach.
+    int vko[kBlocks], vvo[kBlocks];
 #pragma unroll
-        for (int i = 0; i < kBlocks; ++i) {
-            const int r = (wave * kBlocks + i) * kBlockRows + lane / W::kChunks;
-            const int c = ((lane % W::kChunks) ^ W::swz(r)) * 16;
-            vko[i] = r * a.ldk * kEs + c;
-            vvo[i] = r * a.ldv * kEs + c;
+    for (int i = 0; i < kBlocks; ++i) {
+        const int r = (wave * kBlocks + i) * kBlockRows + lane / W::kChunks;
+        const int c = ((lane % W::kChunks) ^ W::swz(r)) * 16;
+        vko[i] = r * a.ldk * kEs + c;
+        vvo[i] = r * a.ldv * kEs + c;
+    }
+    const T* const kbase = static_cast<const T*>(a.k) + first * a.ldk + hk * kHeadDim;
+    const T* const vbase = static_cast<const T*>(a.v) + first * a.ldv + hk * kHeadDim;
+    const int tail_chunk = n / kWinChunk, tail = n % kWinChunk;  // the chunk that the last key cuts
+    const auto issue = [&](int i, int stage) {
+        const int c = chunk(i), valid = c == tail_chunk ? tail : kWinChunk;
+        const __amdgpu_buffer_rsrc_t rk = chunk_rsrc(kbase + (int64_t)c * (kWinChunk * a.ldk), (uint32_t)(valid * a.ldk) * kEs);
+        const __amdgpu_buffer_rsrc_t rv = chunk_rsrc(vbase + (int64_t)c * (kWinChunk * a.ldv), (uint32_t)(valid * a.ldv) * kEs);
+        uint8_t* const st = kvs + stage;
+#pragma unroll
+        for (int i2 = 0; i2 < kBlocks; ++i2) {
+            const int blk = wave * kBlocks + i2;
+            copy_1k(rk, st + blk * 1024, vko[i2]);
+            copy_1k(rv, st + kWinChunk * W::kRow + blk * 1024, vvo[i2]);
         }
-        const T* const kbase = static_cast<const T*>(a.k) + first * a.ldk + hk * kHeadDim;
-        const T* const vbase = static_cast<const T*>(a.v) + first * a.ldv + hk * kHeadDim;
-        const int tail_chunk = n / kWinChunk, tail = n % kWinChunk;  // the chunk that the last key cuts
-        const auto issue = [&](int i, auto stg) {
-            const int c = chunk(i), valid = c == tail_chunk ? tail : kWinChunk;
-            const __amdgpu_buffer_rsrc_t rk = chunk_rsrc(kbase + (int64_t)c * (kWinChunk * a.ldk), (uint32_t)(valid * a.ldk) * kEs);
-            const __amdgpu_buffer_rsrc_t rv = chunk_rsrc(vbase + (int64_t)c * (kWinChunk * a.ldv), (uint32_t)(valid * a.ldv) * kEs);
-            uint8_t* const st = kvs + decltype(stg)::value * kStage;
+    };
+    // Q operand: bf16 k = 16 ks + 8 h2 .. of row l32; fp32 k = 8 u + 4 h2 + e
+    constexpr int kQ = BF16 ? 4 : 8;
+    u32x4 qf[kQ];
+    const T* const qrow = static_cast<const T*>(a.q) + (int64_t)(t0 + tok) * a.ldq + head * kHeadDim;
 #pragma unroll
-            for (int i2 = 0; i2 < kBlocks; ++i2) {
-                const int blk = wave * kBlocks + i2;
-                copy_1k(rk, st + blk * 1024, vko[i2]);
-                copy_1k(rv, st + kWinChunk * W::kRow + blk * 1024, vvo[i2]);
+    for (int u = 0; u < kQ; ++u) {
+        qf[u] = active ? *reinterpret_cast<const u32x4*>(qrow + (BF16 ? 16 * u + 8 * h2 : 8 * u + 4 * h2)) : u32x4{0u, 0u, 0u, 0u};
+        if (flip) qf[u] ^= BF16 ? 0x80008000u : 0x80000000u;
+    }
+    float m = -FLT_MAX, lsum = 0.f;
+    bool fresh = true;  // no chunk yet
+    floatx16 oacc[2];
+#pragma unroll
+    for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[cb][r] = 0.f;
+
+    // One chunk of the stage at byte `stage`; EDGE: some row does not see some key of it.  (Two instances: the tests of
+    // the masks, and the registers they hold, stay out of the chunks that need none.)
+    const auto work = [&](int c, bool whole, auto stg) {
+        constexpr int stage = decltype(stg)::value;
+        const int c0 = c * kWinChunk;
+        const uint8_t* const kst = kvs + stage;
+        const uint8_t* const vst = kst + kWinChunk * W::kRow;
+        const auto visible = [&](int r) {  // the key of accumulator element r
+            const int j = c0 + 4 * h2 + 8 * (r / 4) + (r % 4);
+            return ((uint32_t)(j - from) < range) | (j < sink_range);
+        };
+        floatx16 acc;
+        // (LEAN: a K fragment at a time, for the rare recomputation, where V is already held)
+        const auto products = [&](auto lean) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+            if constexpr (BF16) {
+                const uint16_t* const ks = reinterpret_cast<const uint16_t*>(kst);
+                u32x4 kf[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) kf[u] = *reinterpret_cast<const u32x4*>(ks + kv_off(l32, 16 * u + 8 * h2));
+                if constexpr (!decltype(lean)::value) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) acc = mfma32x32x16(as_bf16x8(kf[u]), as_bf16x8(qf[u]), acc);
+            } else {
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const floatx4 kf = *reinterpret_cast<const floatx4*>(kst + l32 * W::kRow + (((2 * u + h2) ^ W::swz(l32)) * 16));
+                    const floatx4 q4 = __builtin_bit_cast(floatx4, qf[u]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc = mfma32x32x2(kf[e], q4[e], acc);
+                }
             }
         };
-        // Q operand: bf16 k = 16 ks + 8 h2 .. of row l32; fp32 k = 8 u + 4 h2 + e
-        u32x4 qf[BF16 ? 4 : 8];
-        {
-            const T* const qrow = static_cast<const T*>(a.q) + (int64_t)(t0 + tok) * a.ldq + head * kHeadDim;
+        const auto hide = [&] {
+            if (!whole) {
 #pragma unroll
-            for (int u = 0; u < (BF16 ? 4 : 8); ++u) {
-                qf[u] = active ? *reinterpret_cast<const u32x4*>(qrow + (BF16 ? 16 * u + 8 * h2 : 8 * u + 4 * h2))
-                               : u32x4{0u, 0u, 0u, 0u};
-                if (flip) qf[u] ^= BF16 ? 0x80008000u : 0x80000000u;
+                for (int r = 0; r < 16; ++r) acc[r] = visible(r) ? acc[r] : -INFINITY;
+            }
+        };
+        const auto chunk_max = [&] {
+            float cmax = acc[0];
+#pragma unroll
+            for (int r = 1; r < 16; ++r) cmax = fmaxf(cmax, acc[r]);
+            return max_xor32(cmax) * zs;
+        };
+        const auto exps = [&] {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[r] = __builtin_amdgcn_exp2f(fmaf(acc[r], zs, -m));
+            float s[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) s[r] = acc[2 * r] + acc[2 * r + 1];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[r] += s[r + 4];
+            return (s[0] + s[2]) + (s[1] + s[3]);
+        };
+        products(std::false_type{});
+        // V^T operand: the lane's keys 16 t + {4 h2 .. + 3, 8 + 4 h2 .. + 3} of channel 32 cb + l32, by transposed
+        // reads whose latency passes under the products above (inline assembly, its own wait
+        // included: at the builtin the compiler waits for every copy into LDS, the next chunk's
+        // too)
+        u32x2 tr[2][2][2];
+        if constexpr (BF16) {
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile(
+                "ds_read_b64_tr_b16 %0, %8 offset:%12\n\t"
+                "ds_read_b64_tr_b16 %1, %9 offset:%12\n\t"
+                "ds_read_b64_tr_b16 %2, %10 offset:%12\n\t"
+                "ds_read_b64_tr_b16 %3, %11 offset:%12\n\t"
+                "ds_read_b64_tr_b16 %4, %8 offset:%13\n\t"
+                "ds_read_b64_tr_b16 %5, %9 offset:%13\n\t"
+                "ds_read_b64_tr_b16 %6, %10 offset:%13\n\t"
+                "ds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
+                "s_waitcnt lgkmcnt(0)"
+                : "=&v"(tr[0][0][0]), "=&v"(tr[0][0][1]), "=&v"(tr[0][1][0]), "=&v"(tr[0][1][1]),
+                  "=&v"(tr[1][0][0]), "=&v"(tr[1][0][1]), "=&v"(tr[1][1][0]), "=&v"(tr[1][1][1])
+                : "v"(vaddr[0][0]), "v"(vaddr[0][1]), "v"(vaddr[1][0]), "v"(vaddr[1][1]),
+                  "i"(stage + kWinChunk * W::kRow), "i"(stage + kWinChunk * W::kRow + 16 * W::kRow)
+                : "memory");
+        }
+        hide();
+        if (fresh) m = fmaxf(chunk_max(), -FLT_MAX);  // (no visible key: any later score is far above)
+        float ps = exps();
+        // a lane sum above kSumCap (or NaN) means a score well above m: raise m to the
+        // chunk's maximum and rescale what has been summed
+        if (!fresh && __ballot(!(ps <= kSumCap)) != 0) {
+            products(std::true_type{});
+            hide();
+            const float mn = fmaxf(m, chunk_max());
+            const float alpha = __builtin_amdgcn_exp2f(m - mn);
+            lsum *= alpha;
+#pragma unroll
+            for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) oacc[cb][r] *= alpha;
+            m = mn;
+            ps = exps();
+        }
+        fresh = false;
+        lsum += ps;
+        // Values that are not finite, among hidden keys: taken out of the operand, and added to the rows
+        // that see them (a positive weight leaves an infinity or NaN what it is): a row's products
+        // of what it sees (1 or 0) with where V is +infinity or NaN, and -infinity or NaN.
+        const auto add_infinite = [&](floatx16 count, int cb, float inf) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) oacc[cb][r] += count[r] > 0.f ? inf : 0.f;
+        };
+        floatx16 zero;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) zero[r] = 0.f;
+        if constexpr (BF16) {
+            const auto operand = [&](int t, int cb, auto f) {
+                return as_bf16x8(u32x4{f(tr[t][cb][0][0]), f(tr[t][cb][0][1]), f(tr[t][cb][1][0]), f(tr[t][cb][1][1])});
+            };
+            if (!whole) {
+                uint32_t bad = 0;  // an exponent of all ones in either half
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    bad |= ((tr[e >> 3][e >> 2 & 1][e >> 1 & 1][e & 1] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+                if (__ballot(bad != 0) != 0) {
+                    u32x4 vis[2];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        vis[e / 4][e % 4] = (visible(2 * e) ? 0x3f80u : 0u) | (visible(2 * e + 1) ? 0x3f800000u : 0u);
+#pragma unroll
+                    for (int sign = 0; sign < 2; ++sign) {
+                        const uint32_t other = sign ? 0x7f80u : 0xff80u;  // the other sign's infinity
+                        const auto where = [&](uint32_t x) {
+                            const uint32_t lo = x & 0xffffu, hi = x >> 16;
+                            return ((lo & 0x7f80u) == 0x7f80u && lo != other ? 0x3f80u : 0u) |
+                                   ((hi & 0x7f80u) == 0x7f80u && hi != other ? 0x3f800000u : 0u);
+                        };
+#pragma unroll
+                        for (int cb = 0; cb < 2; ++cb) {
+                            floatx16 n = mfma32x32x16(operand(0, cb, where), as_bf16x8(vis[0]), zero);
+                            n = mfma32x32x16(operand(1, cb, where), as_bf16x8(vis[1]), n);
+                            add_infinite(n, cb, sign ? -INFINITY : INFINITY);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        uint32_t x = tr[e >> 3][e >> 2 & 1][e >> 1 & 1][e & 1];
+                        if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+                        if ((x & 0x7f800000u) == 0x7f800000u) x &= 0x0000ffffu;
+                        tr[e >> 3][e >> 2 & 1][e >> 1 & 1][e & 1] = x;
+                    }
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                u32x4 pw;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) pw[e] = pack_bf16x2(acc[8 * t + 2 * e], acc[8 * t + 2 * e + 1]);
+#pragma unroll
+                for (int cb = 0; cb < 2; ++cb)
+                    oacc[cb] = mfma32x32x16(operand(t, cb, [](uint32_t x) { return x; }), as_bf16x8(pw), oacc[cb]);
+            }
+        } else {
+            // the lane's keys 8 (r / 4) + 4 h2 + r % 4 of channel 32 cb + l32
+            float vf[2][16];
+            bool bad = false;
+#pragma unroll
+            for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int kk = 8 * (r / 4) + 4 * h2 + (r % 4), ch = 32 * cb + l32;
+                    vf[cb][r] = *reinterpret_cast<const float*>(vst + kk * W::kRow + (((ch >> 2) ^ W::swz(kk)) * 16) + (ch & 3) * 4);
+                    bad |= !finite_f32(vf[cb][r]);
+                }
+            if (!whole && __ballot(bad) != 0) {
+#pragma unroll
+                for (int sign = 0; sign < 2; ++sign)
+#pragma unroll
+                    for (int cb = 0; cb < 2; ++cb) {
+                        floatx16 n = zero;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const float x = vf[cb][r];
+                            n = mfma32x32x2(!finite_f32(x) && x != (sign ? INFINITY : -INFINITY) ? 1.f : 0.f, visible(r) ? 1.f : 0.f, n);
+                        }
+                        add_infinite(n, cb, sign ? -INFINITY : INFINITY);
+                    }
+#pragma unroll
+                for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (!finite_f32(vf[cb][r])) vf[cb][r] = 0.f;
+            }
+            // groups of eight keys; those that no row of the wave sees are left out (a chunk of four sinks
+            // is two thirds of one)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int k0 = c0 + 8 * g;
+                if (k0 > phi || (k0 + 7 < wfrom && k0 >= a.sinks)) continue;
+#pragma unroll
+                for (int r = 4 * g; r < 4 * g + 4; ++r)
+#pragma unroll
+                    for (int cb = 0; cb < 2; ++cb) oacc[cb] = mfma32x32x2(vf[cb][r], acc[r], oacc[cb]);
             }
         }
-        float m = -FLT_MAX, lsum = 0.f;
-        bool fresh = true;  // no chunk yet
-        floatx16 oacc[2];
+    };
+    const auto step = [&](int i, auto stg) {
+        constexpr int stage = decltype(stg)::value;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's copies of chunk i
+        attn_barrier();  // ... and the other wave's; the other stage was last read in step i - 1
+        if (i + 1 < i1) issue(i + 1, stage ^ kStage);
+        const int c = chunk(i);
+        if (c > last || (c < wfirst && c >= sinks1)) return;  // no row of the wave sees a key of it
+        work(c, c >= whole0 && c < whole1, stg);
+    };
+    if (i0 < i1) issue(i0, 0);
+    for (int i = i0; i < i1; i += 2) {
+        step(i, std::integral_constant<int, 0>{});
+        if (i + 1 < i1) step(i + 1, std::integral_constant<int, kStage>{});
+    }
+    float sum = sum_xor32(lsum);
+    if (r0 + w0 + l32 >= rows) return;
+    if (p < 0 || (a.window == 0 && a.sinks == 0)) sum = 1.f;  // the row sees nothing: its output is zero
+    const int64_t gr = (int64_t)(t0 + tok);
+    if (a.splits > 1) {
+        const int64_t slot = ((int64_t)blockIdx.y * a.T + gr) * a.heads + head;
+        float* const po = a.part_o + slot * kHeadDim;
 #pragma unroll
         for (int cb = 0; cb < 2; ++cb)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) oacc[cb][r] = 0.f;
-
-        const auto step = [&](int i, auto stg) {
-            constexpr int STG = decltype(stg)::value;
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's copies of chunk i
-            attn_barrier();  // ... and the other wave's; the other stage was last read in step i - 1
-            if (i + 1 < i1) issue(i + 1, std::integral_constant<int, 1 - STG>{});
-            const int c = chunk(i), c0 = c * kWinChunk;
-            if (c > last || (c < wfirst && c >= sinks1)) return;  // no row of the wave sees a key of it
-            const bool whole = c < whole1 && (c >= whole0 || c < sinks0);
-            const uint8_t* const kst = kvs + STG * kStage;
-            const uint8_t* const vst = kst + kWinChunk * W::kRow;
-            const auto visible = [&](int j) { return ((uint32_t)(j - from) < range) | ((j < a.sinks) & (j <= p)); };
-            floatx16 acc;
-            // (LEAN: a K fragment at a time, for the rare recomputation, where V is already held)
-            const auto products = [&](auto lean) {
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<floatx4*>(po + 32 * cb + 8 * g + 4 * h2) =
+                    floatx4{oacc[cb][4 * g], oacc[cb][4 * g + 1], oacc[cb][4 * g + 2], oacc[cb][4 * g + 3]};
+        if (h2 == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * slot) = float2{m, sum};
+    } else {
+        const float inv = 1.0f / sum;
+        T* const orow = static_cast<T*>(a.out) + gr * a.ldo + head * kHeadDim;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[r] = 0.f;
-                if constexpr (BF16) {
-                    const uint16_t* const ks = reinterpret_cast<const uint16_t*>(kst);
-                    u32x4 kf[4];
+        for (int cb = 0; cb < 2; ++cb)
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) kf[u] = *reinterpret_cast<const u32x4*>(ks + kv_off(l32, 16 * u + 8 * h2));
-                    if constexpr (!decltype(lean)::value) __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) acc = mfma32x32x16(as_bf16x8(kf[u]), as_bf16x8(qf[u]), acc);
-                } else {
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-                        const floatx4 kf = *reinterpret_cast<const floatx4*>(kst + l32 * W::kRow + (((2 * u + h2) ^ W::swz(l32)) * 16));
-                        const floatx4 q4 = __builtin_bit_cast(floatx4, qf[u]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc = mfma32x32x2(kf[e], q4[e], acc);
-                    }
-                }
-            };
-            const auto hide = [&] {
-                if (!whole) {
-                    if (c >= sinks1) {
-                        const int j0 = c0 + 4 * h2 - from;
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            acc[r] = (uint32_t)(j0 + 8 * (r / 4) + (r % 4)) < range ? acc[r] : -INFINITY;
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            acc[r] = visible(c0 + 4 * h2 + 8 * (r / 4) + (r % 4)) ? acc[r] : -INFINITY;
-                    }
-                }
-            };
-            const auto chunk_max = [&] {
-                float cmax = acc[0];
-#pragma unroll
-                for (int r = 1; r < 16; ++r) cmax = fmaxf(cmax, acc[r]);
-                return max_xor32(cmax) * zs;
-            };
-            const auto exps = [&] {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) acc[r] = __builtin_amdgcn_exp2f(fmaf(acc[r], zs, -m));
-                float s[8];
-#pragma unroll
-                for (int r = 0; r < 8; ++r) s[r] = acc[2 * r] + acc[2 * r + 1];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[r] += s[r + 4];
-                return (s[0] + s[2]) + (s[1] + s[3]);
-            };
-            products(std::false_type{});
-            // V^T operand: the lane's keys 16 t + {4 h2 .. + 3, 8 + 4 h2 .. + 3} of channel 32 cb + l32, by transposed
-            // reads whose latency passes under the products above (inline assembly, its own wait
-            // included: at the builtin the compiler waits for every copy into LDS, the next chunk's
-            // too)
-            u32x2 tr[2][2][2];
-            if constexpr (BF16) {
-                __builtin_amdgcn_sched_barrier(0);
-                asm volatile(
-                    "ds_read_b64_tr_b16 %0, %8 offset:%12\n\t"
-                    "ds_read_b64_tr_b16 %1, %9 offset:%12\n\t"
-                    "ds_read_b64_tr_b16 %2, %10 offset:%12\n\t"
-                    "ds_read_b64_tr_b16 %3, %11 offset:%12\n\t"
-                    "ds_read_b64_tr_b16 %4, %8 offset:%13\n\t"
-                    "ds_read_b64_tr_b16 %5, %9 offset:%13\n\t"
-                    "ds_read_b64_tr_b16 %6, %10 offset:%13\n\t"
-                    "ds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
-                    "s_waitcnt lgkmcnt(0)"
-                    : "=&v"(tr[0][0][0]), "=&v"(tr[0][0][1]), "=&v"(tr[0][1][0]), "=&v"(tr[0][1][1]),
-                      "=&v"(tr[1][0][0]), "=&v"(tr[1][0][1]), "=&v"(tr[1][1][0]), "=&v"(tr[1][1][1])
-                    : "v"(vaddr[0][0]), "v"(vaddr[0][1]), "v"(vaddr[1][0]), "v"(vaddr[1][1]),
-                      "i"(STG * kStage + kWinChunk * W::kRow), "i"(STG * kStage + kWinChunk * W::kRow + 16 * W::kRow)
-                    : "memory");
+            for (int g = 0; g < 4; ++g) {
+                const float o0 = oacc[cb][4 * g] * inv, o1 = oacc[cb][4 * g + 1] * inv, o2 = oacc[cb][4 * g + 2] * inv,
+                            o3 = oacc[cb][4 * g + 3] * inv;
+                if constexpr (BF16)
+                    *reinterpret_cast<u32x2*>(orow + 32 * cb + 8 * g + 4 * h2) = u32x2{pack_bf16x2(o0, o1), pack_bf16x2(o2, o3)};
+                else
+                    *reinterpret_cast<floatx4*>(orow + 32 * cb + 8 * g + 4 * h2) = floatx4{o0, o1, o2, o3};
             }
-            hide();
-            if (fresh) m = fmaxf(chunk_max(), -FLT_MAX);  // (no visible key: any later score is far above)
-            float ps = exps();
-            // a lane sum above kSumCap (or NaN) means a score well above m: raise m to the
-            // chunk's maximum and rescale what has been summed
-            if (!fresh && __ballot(!(ps <= kSumCap)) != 0) {
-                products(std::true_type{});
-                hide();
-                const float mn = fmaxf(m, chunk_max());
-                const float alpha = __builtin_amdgcn_exp2f(m - mn);
-                lsum *= alpha;
-#pragma unroll
-                for (int cb = 0; cb < 2; ++cb)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) oacc[cb][r] *= alpha;
-                m = mn;
-                ps = exps();
-            }
-            fresh = false;
-            lsum += ps;
-            // values that are not finite, in a chunk with hidden keys: added to the rows that
-            // see them (a positive weight leaves an infinity or NaN what it is)
-            const auto add_seen = [&](auto value) {
-                for (int kk = 0; kk < kWinChunk; ++kk) {
-                    if (!visible(c0 + kk)) continue;
-#pragma unroll
-                    for (int cb = 0; cb < 2; ++cb)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const float x = value(kk, 32 * cb + 8 * (r / 4) + 4 * h2 + (r % 4));
-                            if (!finite_f32(x)) oacc[cb][r] += x;
-                        }
-                }
-            };
-            if constexpr (BF16) {
-                const uint16_t* const vs = reinterpret_cast<const uint16_t*>(vst);
-                if (!whole) {
-                    bool bad = false;
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-#pragma unroll
-                        for (int cb = 0; cb < 2; ++cb)
-#pragma unroll
-                            for (int hi = 0; hi < 2; ++hi)
-#pragma unroll
-                                for (int w = 0; w < 2; ++w) {
-                                    const uint32_t x = tr[t][cb][hi][w];
-                                    bad |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
-                                }
-                    if (__ballot(bad) != 0) {
-#pragma unroll
-                        for (int t = 0; t < 2; ++t)
-#pragma unroll
-                            for (int cb = 0; cb < 2; ++cb)
-#pragma unroll
-                                for (int hi = 0; hi < 2; ++hi)
-#pragma unroll
-                                    for (int w = 0; w < 2; ++w) {
-                                        uint32_t x = tr[t][cb][hi][w];
-                                        if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
-                                        if ((x & 0x7f800000u) == 0x7f800000u) x &= 0x0000ffffu;
-                                        tr[t][cb][hi][w] = x;
-                                    }
-                        add_seen([&](int kk, int ch) { return bf16_to_f32(vs[kv_off(kk, ch)]); });
-                    }
-                }
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    u32x4 pw;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) pw[e] = pack_bf16x2(acc[8 * t + 2 * e], acc[8 * t + 2 * e + 1]);
-                    const bf16x8 pb = as_bf16x8(pw);
-#pragma unroll
-                    for (int cb = 0; cb < 2; ++cb)
-                        oacc[cb] = mfma32x32x16(
-                            as_bf16x8(u32x4{tr[t][cb][0][0], tr[t][cb][0][1], tr[t][cb][1][0], tr[t][cb][1][1]}), pb, oacc[cb]);
-                }
-            } else {
-                const auto value = [&](int kk, int ch) {
-                    return *reinterpret_cast<const float*>(vst + kk * W::kRow + (((ch >> 2) ^ W::swz(kk)) * 16) + (ch & 3) * 4);
-                };
-                float vf[2][16];
-                bool bad = false;
-#pragma unroll
-                for (int cb = 0; cb < 2; ++cb)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        vf[cb][r] = value(8 * (r / 4) + 4 * h2 + (r % 4), 32 * cb + l32);
-                        bad |= !finite_f32(vf[cb][r]);
-                    }
-                if (!whole && __ballot(bad) != 0) {
-#pragma unroll
-                    for (int cb = 0; cb < 2; ++cb)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (!finite_f32(vf[cb][r])) vf[cb][r] = 0.f;
-                    add_seen(value);
-                }
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-#pragma unroll
-                    for (int cb = 0; cb < 2; ++cb)
-                        oacc[cb] = mfma32x32x2(vf[cb][r], acc[r], oacc[cb]);
-            }
-        };
-        attn_barrier();  // both stages are free: the previous item's reads are done
-        if (i0 < i1) issue(i0, std::integral_constant<int, 0>{});
-        for (int i = i0; i < i1; i += 2) {
-            step(i, std::integral_constant<int, 0>{});
-            if (i + 1 < i1) step(i + 1, std::integral_constant<int, 1>{});
-        }
-        if (!active || w0 + l32 >= rows) continue;
-        float sum = sum_xor32(lsum);
-        const bool empty = p < 0 || (a.window == 0 && a.sinks == 0);
-        if (empty) sum = 1.f;  // (its output is zero)
-        const int64_t gr = (int64_t)(t0 + tok);
-        if (a.splits > 1) {
-            const int64_t slot = ((int64_t)blockIdx.y * a.T + gr) * a.heads + head;
-            float* const po = a.part_o + slot * kHeadDim;
-#pragma unroll
-            for (int cb = 0; cb < 2; ++cb)
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *reinterpret_cast<floatx4*>(po + 32 * cb + 8 * g + 4 * h2) =
-                        floatx4{oacc[cb][4 * g], oacc[cb][4 * g + 1], oacc[cb][4 * g + 2], oacc[cb][4 * g + 3]};
-            if (h2 == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * slot) = float2{m, sum};
-        } else {
-            const float inv = 1.0f / sum;
-            T* const orow = static_cast<T*>(a.out) + gr * a.ldo + head * kHeadDim;
-#pragma unroll
-            for (int cb = 0; cb < 2; ++cb)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const float o0 = oacc[cb][4 * g] * inv, o1 = oacc[cb][4 * g + 1] * inv, o2 = oacc[cb][4 * g + 2] * inv,
-                                o3 = oacc[cb][4 * g + 3] * inv;
-                    if constexpr (BF16)
-                        *reinterpret_cast<u32x2*>(orow + 32 * cb + 8 * g + 4 * h2) = u32x2{pack_bf16x2(o0, o1), pack_bf16x2(o2, o3)};
-                    else
-                        *reinterpret_cast<floatx4*>(orow + 32 * cb + 8 * g + 4 * h2) = floatx4{o0, o1, o2, o3};
-                }
-        }
     }
 }
 
-// Joins the splits' states of one (token, head) row per workgroup: sixteen lanes of four channels
-// each take every sixteenth split, all their loads in flight at once.
-constexpr int kWinMaxSplits = 256, kJoinGroups = 16;
+// Joins the splits' states of a (token, head) row: sixteen lanes of four channels each, all
+// their PER loads in flight at once.  GROUPS = 16: one row per workgroup, whose sixteen groups take every
+// sixteenth split; GROUPS = 1: sixteen rows.
+constexpr int kWinMaxSplits = 256;
 
-template <bool BF16>
+template <bool BF16, int GROUPS, int PER>
 __global__ __launch_bounds__(256) void k_attention_window_join(WinArgs a) {
     if (a.status[0] != 0) return;
     using T = typename WinT<BF16>::T;
-    constexpr int kPer = kWinMaxSplits / kJoinGroups;
     __shared__ float wmax[4], wsum[4];
     __shared__ __attribute__((aligned(16))) float wout[4][kHeadDim];
-    const int64_t rows = (int64_t)a.T * a.heads, r = blockIdx.x;
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, g = threadIdx.x / 16, c = lane % 16 * 4;
-    float ms[kPer], ls[kPer], m = -FLT_MAX;
-    floatx4 o = {0.f, 0.f, 0.f, 0.f}, os[kPer];
-    const int n = (a.splits - g + kJoinGroups - 1) / kJoinGroups;  // this group's splits (may be none)
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, c = lane % 16 * 4;
+    const int64_t rows = (int64_t)a.T * a.heads;
+    const int64_t r = GROUPS == 1 ? (int64_t)blockIdx.x * 16 + threadIdx.x / 16 : blockIdx.x;
+    const int g = GROUPS == 1 ? 0 : threadIdx.x / 16;
+    if (r >= rows) return;  // (GROUPS == 1 only, which never synchronises)
+    float ms[PER], ls[PER], m = -FLT_MAX;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f}, os[PER];
+    const int n = (a.splits - g + GROUPS - 1) / GROUPS;  // this group's splits (may be none); indexes past them are clamped
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        if (i * kJoinGroups >= a.splits) break;
-        const int64_t slot = (int64_t)min(g + i * kJoinGroups, a.splits - 1) * rows + r;
+    for (int i = 0; i < PER; ++i) {
+        const int64_t slot = (int64_t)min(g + i * GROUPS, a.splits - 1) * rows + r;
         const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * slot);
         os[i] = *reinterpret_cast<const floatx4*>(a.part_o + slot * kHeadDim + c);
         ms[i] = ml.x;
         ls[i] = ml.y;
-        m = fmaxf(m, ml.x);
     }
-    m = wave_max(m);
-    if (lane == 0) wmax[wave] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(wmax[0], wmax[1]), fmaxf(wmax[2], wmax[3]));
+#pragma unroll
+    for (int i = 0; i < PER; ++i) m = fmaxf(m, ms[i]);
+    if constexpr (GROUPS > 1) {
+        m = wave_max(m);
+        if (lane == 0) wmax[wave] = m;
+        __syncthreads();
+        m = fmaxf(fmaxf(wmax[0], wmax[1]), fmaxf(wmax[2], wmax[3]));
+    }
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        if (i >= n) break;
-        const float w = __builtin_amdgcn_exp2f(ms[i] - m);
+    for (int i = 0; i < PER; ++i) {
+        const float w = i < n ? __builtin_amdgcn_exp2f(ms[i] - m) : 0.f;
         sum = fmaf(w, ls[i], sum);
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] = fmaf(w, os[i][e], o[e]);
     }
-    // the wave's four groups, then the four waves
+    if constexpr (GROUPS > 1) {  // the wave's four groups, then the four waves
 #pragma unroll
-    for (int d = 16; d <= 32; d *= 2) {
-        sum += __shfl_xor(sum, d);
+        for (int d = 16; d <= 32; d *= 2) {
+            sum += __shfl_xor(sum, d);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], d);
+            for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], d);
+        }
+        if (lane < 16) *reinterpret_cast<floatx4*>(&wout[wave][c]) = o;
+        if (lane == 0) wsum[wave] = sum;
+        __syncthreads();
+        if (threadIdx.x >= 16) return;
+        sum = wsum[0] + wsum[1] + wsum[2] + wsum[3];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = wout[0][c + e] + wout[1][c + e] + wout[2][c + e] + wout[3][c + e];
     }
-    if (lane < 16) *reinterpret_cast<floatx4*>(&wout[wave][c]) = o;
-    if (lane == 0) wsum[wave] = sum;
-    __syncthreads();
-    if (threadIdx.x >= kHeadDim) return;
-    const float v = (wout[0][lane] + wout[1][lane] + wout[2][lane] + wout[3][lane]) / (wsum[0] + wsum[1] + wsum[2] + wsum[3]);
-    T* const dst = static_cast<T*>(a.out) + (r / a.heads) * a.ldo + (r % a.heads) * kHeadDim + lane;
-    if constexpr (BF16) *dst = f32_to_bf16(v);
-    else *dst = v;
+    const float inv = 1.0f / sum;
+    T* const dst = static_cast<T*>(a.out) + (r / a.heads) * a.ldo + (r % a.heads) * kHeadDim + c;
+    if constexpr (BF16) *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
+    else *reinterpret_cast<floatx4*>(dst) = floatx4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
 }
 
 }  // namespace
@@ -526,10 +556,23 @@ size_t window_workspace(int64_t T, int64_t heads, int64_t splits) {
     return splits > 1 ? (size_t)(splits * T * heads * (kHeadDim + 2)) * sizeof(float) : 0;
 }
 
+namespace {
+template <bool BF16>
+void launch_join(const WinArgs& a, int splits, int64_t rows, hipStream_t s) {
+    const bool few = splits <= 16;
+    const int per = few ? splits : (splits + 15) / 16;
+    auto* f = few ? (per <= 2 ? &k_attention_window_join<BF16, 1, 2> : per <= 4 ? &k_attention_window_join<BF16, 1, 4>
+                     : per <= 8 ? &k_attention_window_join<BF16, 1, 8> : &k_attention_window_join<BF16, 1, 16>)
+                  : (per <= 2 ? &k_attention_window_join<BF16, 16, 2> : per <= 4 ? &k_attention_window_join<BF16, 16, 4>
+                     : per <= 8 ? &k_attention_window_join<BF16, 16, 8> : &k_attention_window_join<BF16, 16, 16>);
+    hipLaunchKernelGGL(f, dim3((unsigned)(few ? (rows + 15) / 16 : rows)), dim3(256), 0, s, a);
+}
+}  // namespace
+
 hipError_t launch_attention_window(const PlanView& p, int dtype, const void* q, int ldq, const void* k, int ldk,
                                    const void* v, int ldv, const WindowKeys& keys, int kv_heads, float scale, int window,
                                    int sinks, void* out, int ldo, int splits, void* workspace, hipStream_t s) {
-    if (p.total_tokens == 0) return hipSuccess;
+    if (p.total_tokens == 0 || p.av_cap == 0) return hipSuccess;  // (no entries: nothing can be written)
     float* const ws = static_cast<float*>(workspace);
     const int64_t rows = (int64_t)p.total_tokens * p.heads;
     // Where every sequence's rows of a key head fill one tile (a step of single tokens), only
@@ -539,19 +582,19 @@ hipError_t launch_attention_window(const PlanView& p, int dtype, const void* q, 
     const int group = p.heads / kv_heads;
     const bool single = (int64_t)p.max_len * group <= kTile;
     const int stride = single ? group : 1, dealt = !single && splits == 1;
-    const WinArgs a{p.lengths, p.tok_off, p.av_items, p.status, keys.first, keys.len, keys.rows, keys.max_len, q, k, v, out,
-                    ldq, ldk, ldv, ldo, p.heads, group, window, sinks, scale, p.total_tokens, splits, stride, dealt, ws,
+    const WinArgs a{p.lengths, p.tok_off, p.av_items, p.av_cap, p.status, keys.first, keys.len, keys.rows, keys.max_len, q, k, v, out,
+                    ldq, ldk, ldv, ldo, p.heads, group, group == 1 ? 0u : (uint32_t)(0xffffffffu / (uint32_t)group + 1), window, sinks, scale, p.total_tokens, splits, stride, dealt, ws,
                     ws ? ws + (int64_t)splits * rows * kHeadDim : nullptr};
-    constexpr int64_t kUnit = 8 * kStreamRun;
-    const int64_t cap = std::max<int64_t>(p.av_cap / stride, 1), limit = (int64_t)device_cu_count() * kWinPerCu;
-    const int64_t g = dealt ? (std::min(cap, limit) + kUnit - 1) / kUnit * kUnit : std::min(cap, limit);
-    const dim3 grid((unsigned)g, (unsigned)splits);
-    if (dtype == 1) hipLaunchKernelGGL(k_attention_window<true>, grid, dim3(kWinThreads), 0, s, a);
-    else hipLaunchKernelGGL(k_attention_window<false>, grid, dim3(kWinThreads), 0, s, a);
+    // one workgroup per entry that a plan of this capacity can hold (in rows of 2^20)
+    constexpr int64_t kUnit = 8 * kStreamRun, kRow = 1 << 20;
+    int64_t g = std::max<int64_t>(p.av_cap / stride, 1);
+    if (dealt) g = (g + kUnit - 1) / kUnit * kUnit;  // dealing is a permutation of these
+    const dim3 grid((unsigned)std::min(g, kRow), (unsigned)splits, (unsigned)((g + kRow - 1) / kRow));
+    auto* f = dtype == 1 ? &k_attention_window<true> : &k_attention_window<false>;
+    hipLaunchKernelGGL(f, grid, dim3(kWinThreads), 0, s, a);
     if (splits > 1) {
-        const dim3 jg((unsigned)rows);
-        if (dtype == 1) hipLaunchKernelGGL(k_attention_window_join<true>, jg, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL(k_attention_window_join<false>, jg, dim3(256), 0, s, a);
+        if (dtype == 1) launch_join<true>(a, splits, rows, s);
+        else launch_join<false>(a, splits, rows, s);
     }
     return hipGetLastError();
 }
