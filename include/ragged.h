@@ -455,7 +455,7 @@ rag_status encoder_layer_noalloc(const rag_plan* plan, const void* x, void* y, i
  * The operators of a decoder layer with 8-bit projections.  They read and write
  * packed activations like the operators above (dtype RAG_BF16 or RAG_F32) and
  * hold sums, statistics and softmax states in fp32 (products of 8-bit integers in
- * int32, exactly; angles in fp64).  T, N and plan->total_tokens are at most 2^30.
+ * int32, exactly; angles in fp64).  T, N and plan->total_tokens are at most 2^24.
  *
  * 8-bit rows: row t of an [rows, d] matrix is int8 q and one fp32 scale, its values
  * q[t][c] * scale[t], with scale[t] = max_c |y[t][c]| / 127 and q = y / scale rounded
@@ -560,15 +560,15 @@ rag_status packed_linear_i8(const int8_t* x, int32_t ldx, const float* x_scale, 
  * ragged_attention_window: k and v are the packed batch's own rows [T, kv_heads * hd].
  * ragged_attention_window_cached: k and v are caches of kv_rows rows; sequence b's
  * keys are rows kv_first[b] .. kv_first[b] + kv_len[b] - 1 (int64 and int32 [B], device
- * memory; 0 <= kv_len[b] <= max_kv_len), and its L_b queries are the last L_b of those
+ * memory; 0 <= kv_len[b] <= max_kv_len <= 2^30), and its L_b queries are the last L_b of those
  * kv_len[b] positions: one per sequence for a step of single tokens.  A query before
  * position 0 (L_b > kv_len[b]) sees nothing and gets zeros.  Sequences may
  * share rows.  Rows outside a sequence's range are not read.  A range that leaves the
  * cache sets RAG_DATA_KV_RANGE; the call's outputs are then unspecified.
  *
  * q and out are [T, H * hd]; q, k, v and out are 16-byte aligned with rows that are
- * multiples of 16 bytes, below 2^22 elements.  Keys and values that a position does not see never
- * reach its output, infinities and NaN among them.  `workspace` (16-byte aligned) holds at least the
+ * multiples of 16 bytes, below 2^22 elements; out overlaps nothing.  H is at most 32768.  Keys and
+ * values that a position does not see never reach its output, infinities and NaN among them.  `workspace` (16-byte aligned) holds at least the
  * bytes that ragged_attention_window_workspace gives for the same host values, used when few
  * rows over many keys are split; it needs no clearing, and calls that overlap in time
  * need one each.  (max_kv_len is max_len for ragged_attention_window.)

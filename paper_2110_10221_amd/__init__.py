@@ -290,7 +290,7 @@ def _mat(name, t, shape, dtype, dev):
     if t is None:
         return 0
     ld = t.stride()
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or ld[1] != 1:
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or ld[1] != 1 or ld[0] > 0x7fffffff:
         _refuse(name, t, shape, dtype, dev)
     return ld[0]
 
@@ -308,12 +308,15 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
-def _launch_stream(stream, dev):
-    """The stream to launch on: tensors of another device than the current one are refused."""
-    if dev < 0 or dev != torch.cuda.current_device():
-        raise ValueError("the tensors must be on the current device")
+def _launch_stream(stream, dev, plan=None):
+    """The stream to launch on: tensors (and plans) of another device than the current one are refused."""
+    if dev < 0 or dev != torch.cuda.current_device() or (plan is not None and plan.status.get_device() != dev):
+        raise ValueError("the tensors and the plan must be on the current device")
     # (the current stream's handle; building the Stream object takes longer than the call)
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+_I32_MAX = 2 ** 31 - 1  # (ctypes would wrap a larger window; no position passes it)
 
 
 def packed_rmsnorm(x, gamma, y=None, eps=1e-6, residual=None, x_out=None, q=None, q_scale=None, stream=None):
@@ -375,7 +378,7 @@ def packed_rotary(plan: Plan, x, y, inv_freq, heads, head_dim=RAG_HEAD_DIM, layo
     st = _c_rotary(plan.ref(), x.data_ptr(), _mat("x", x, shape, dt, dev), y.data_ptr(), _mat("y", y, shape, dt, dev), heads,
                    head_dim, 2 * n, layout | (RAG_ROTARY_INVERSE if inverse else 0),
                    _vec("inv_freq", inv_freq, n, torch.float64, dev), amplitude,
-                   _vec("pos_start", pos_start, plan.batch, torch.int32, dev), _dtype_code(x), _launch_stream(stream, dev))
+                   _vec("pos_start", pos_start, plan.batch, torch.int32, dev), _dtype_code(x), _launch_stream(stream, dev, plan))
     if st:
         _check("packed_rotary", st)
 
@@ -384,8 +387,8 @@ def ragged_attention_window_workspace(plan: Plan, max_kv_len, window, sinks=0, k
     """Workspace bytes of the two calls below (max_kv_len: plan.max_len for the first; may be 0)."""
     n = ctypes.c_size_t()
     code = {torch.bfloat16: RAG_BF16, torch.float32: RAG_F32}.get(dtype, -1)
-    _check("ragged_attention_window_workspace", _c_window_ws(plan.ref(), max_kv_len, kv_heads or plan.heads, window, sinks,
-                                                             code, ctypes.byref(n)))
+    _check("ragged_attention_window_workspace", _c_window_ws(plan.ref(), min(max_kv_len, _I32_MAX), kv_heads or plan.heads,
+                                                             min(window, _I32_MAX), min(sinks, _I32_MAX), code, ctypes.byref(n)))
     return n.value
 
 
@@ -407,8 +410,8 @@ def ragged_attention_window(plan: Plan, q, k, v, out, scale, window, sinks=0, kv
     k and v hold kv_heads (default: all) heads, each shared by plan.heads / kv_heads query heads."""
     kvh = kv_heads or plan.heads
     code, dev, ld, ws, n = _window_operands(plan, q, k, v, out, plan.total_tokens, kvh, head_dim, workspace)
-    st = _c_window(plan.ref(), q.data_ptr(), ld[0], k.data_ptr(), ld[1], v.data_ptr(), ld[2], kvh, head_dim, scale, window,
-                   sinks, out.data_ptr(), ld[3], ws, n, code, _launch_stream(stream, dev))
+    st = _c_window(plan.ref(), q.data_ptr(), ld[0], k.data_ptr(), ld[1], v.data_ptr(), ld[2], kvh, head_dim, scale,
+                   min(window, _I32_MAX), min(sinks, _I32_MAX), out.data_ptr(), ld[3], ws, n, code, _launch_stream(stream, dev, plan))
     if st:
         _check("ragged_attention_window", st)
 
@@ -421,8 +424,8 @@ def ragged_attention_window_cached(plan: Plan, q, k, v, kv_first, kv_len, max_kv
     code, dev, ld, ws, n = _window_operands(plan, q, k, v, out, rows, kvh, head_dim, workspace)
     st = _c_window_cached(plan.ref(), q.data_ptr(), ld[0], k.data_ptr(), ld[1], v.data_ptr(), ld[2], rows,
                           _vec("kv_first", kv_first, plan.batch, torch.int64, dev),
-                          _vec("kv_len", kv_len, plan.batch, torch.int32, dev), max_kv_len, kvh, head_dim, scale, window,
-                          sinks, out.data_ptr(), ld[3], ws, n, code, _launch_stream(stream, dev))
+                          _vec("kv_len", kv_len, plan.batch, torch.int32, dev), min(max_kv_len, _I32_MAX), kvh,
+                          head_dim, scale, min(window, _I32_MAX), min(sinks, _I32_MAX), out.data_ptr(), ld[3], ws, n, code, _launch_stream(stream, dev, plan))
     if st:
         _check("ragged_attention_window_cached", st)
 

@@ -610,7 +610,8 @@ rag_status ragged_trmm(const void* l, int32_t ldl, const void* b, int32_t ldb, v
 
 namespace {
 
-constexpr int32_t kMaxRows = 1 << 30;  // row and tile arithmetic of these operators stays in 32 bits
+constexpr int32_t kMaxRows = 1 << 24;  // rows: a launch holds up to 256 threads for each, 2^32 at most
+constexpr int32_t kMaxKeys = 1 << 30;  // keys of a sequence: position arithmetic stays in 32 bits
 
 // Rows read and written in 16-byte chunks in either type.
 rag_status check_rows(const void* ptr, int64_t ld, int64_t width, int32_t dtype, const char* name, const char* fn) {
@@ -820,8 +821,9 @@ rag_status check_window(const rag_plan* plan, rag::PlanView& v, int32_t max_kv_l
     if (kv_heads < 1 || plan->heads % kv_heads != 0)
         return fail(RAG_ERR_SHAPE, "%s: %d heads are not a multiple of %d key heads", fn, plan->heads, kv_heads);
     if (plan->heads > 32768) return fail(RAG_ERR_SHAPE, "%s: more than 32768 heads", fn);
-    if (window < 0 || sinks < 0 || max_kv_len < 0)
-        return fail(RAG_ERR_ARG, "%s: window %d, sinks %d, max_kv_len %d out of range", fn, window, sinks, max_kv_len);
+    if (window < 0 || sinks < 0 || max_kv_len < 0 || max_kv_len > kMaxKeys || plan->total_tokens > kMaxRows)
+        return fail(RAG_ERR_ARG, "%s: window %d, sinks %d, max_kv_len %d or total_tokens %d out of range", fn, window, sinks,
+                    max_kv_len, plan->total_tokens);
     if (((int64_t)plan->total_tokens + RAG_TILE) * (plan->heads / kv_heads) > INT32_MAX)
         return fail(RAG_ERR_SHAPE, "%s: tokens * heads per key head exceed 2^31 - 1", fn);
     return RAG_OK;

@@ -21,9 +21,14 @@
 //           fourth wave per SIMD: six prompts of 1500 to 8192 tokens 172 us, 161 without).
 //   splits  where few rows meet many keys the chunks are dealt to several workgroups
 //           (blockIdx.y), whose (reference, sum, output) states a second launch joins.
-// bf16 rounds the unnormalised exponentials to bf16 for the P V product (a relative 2^-9 of each
-// of many terms, against 2^-9 of the stored result) and nothing else; fp32
+// bf16 rounds the unnormalised exponentials to bf16 for the P V product (a relative 2^-8 at most
+// of each of many terms, beside 2^-8 of the stored result) and nothing else; fp32
 // products run on v_mfma_f32_32x32x2f32 and round nothing.
+// What bounds it: for prompts the exponentials and the vector work around them (16 v_exp_f32
+// of 16 cycles a chunk and wave, about 420 cycles with the sums and conversions, beside 256 of
+// MFMAs that pass under another wave's), in fp32 the 4096 MFMA cycles of a chunk; for single tokens the bytes
+// of K and V: 32 tokens over 4100 keys of 4 heads each, 134 MB, 28.5 us with the join (4.7 TB/s; a
+// large copy reaches 5.2).
 #include <algorithm>
 #include <cfloat>
 #include <type_traits>
@@ -111,7 +116,7 @@ void k_attention_window(WinArgs a) {
     constexpr int kBlockRows = 1024 / W::kRow;             // rows of a 1 KB copy
     constexpr int kBlocks = kWinChunk / kBlockRows / kWinWaves;  // copies of K (and of V) per wave and chunk
     constexpr int kEs = (int)sizeof(T);
-    __shared__ __attribute__((aligned(2 * kStage))) uint8_t kvs[2 * kStage];  // (stages a power of two apart: addresses toggle)
+    __shared__ __attribute__((aligned(16))) uint8_t kvs[2 * kStage];
     const int wave = uni(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int l32 = lane % 32, h2 = lane / 32;
     // (a zero scale would turn hidden keys' -inf into NaN; below 1e-30 every exponential is 1 anyway)
@@ -230,8 +235,8 @@ void k_attention_window(WinArgs a) {
         const uint8_t* const kst = kvs + stage;
         const uint8_t* const vst = kst + kWinChunk * W::kRow;
         floatx16 acc;
-        // (LEAN: a K fragment at a time, for the rare recomputation, where V is already held)
-        const auto products = [&](auto lean) {
+        // (`again`: the rare recomputation, where V is already held and K is read as registers allow)
+        const auto products = [&](auto again) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[r] = 0.f;
             if constexpr (BF16) {
@@ -239,7 +244,7 @@ void k_attention_window(WinArgs a) {
                 u32x4 kf[4];
 #pragma unroll
                 for (int u = 0; u < 4; ++u) kf[u] = *reinterpret_cast<const u32x4*>(ks + kv_off(l32, 16 * u + 8 * h2));
-                if constexpr (!decltype(lean)::value) __builtin_amdgcn_sched_barrier(0);
+                if constexpr (!decltype(again)::value) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int u = 0; u < 4; ++u) acc = mfma32x32x16(as_bf16x8(kf[u]), as_bf16x8(qf[u]), acc);
             } else {
@@ -514,9 +519,9 @@ __global__ __launch_bounds__(256) void k_attention_window_join(WinArgs a) {
 // workgroups to each CU, each with two chunks at least and no more of them than pays for the join: a chunk
 // takes about 0.6 us, the second launch 3 us and 0.07 us a split.  Up to eight chunks that never pays, above
 // the time is least at sqrt(8 chunks) splits.
-// One sequence of 1000 tokens, window 512, 16/4 heads: 13.4 us on two splits, 10.6 on four, 10.1
-// on eight; of 32768 tokens, 8 heads: 18.8 us on 68, 22.1 on 128; 32 sequences, window 4096, 16/4 heads:
-// 32.7 us on eight, 35.8 on 16.  (A whole GPU's 256 CUs: the workspace is sized by the same rule, on the host.)
+// Measured when the rule was made: one sequence of 1000 tokens, window 512, 16/4 heads, 13.4 us on two splits,
+// 10.6 on four, 10.1 on eight; of 32768 tokens, 8 heads, 18.8 us on 68, 22.1 on 128; 32 sequences, window
+// 4096, 16/4 heads, 32.7 us on eight, 35.8 on 16.  (A whole GPU's 256 CUs: the workspace is sized by the same rule, on the host.)
 int window_splits(int64_t T, int64_t batch, int64_t heads, int64_t kv_heads, int64_t max_len, int64_t max_kv, int64_t window,
                   int64_t sinks) {
     if (T <= 0) return 1;
@@ -561,9 +566,10 @@ hipError_t launch_attention_window(const PlanView& p, int dtype, const void* q, 
     const int group = p.heads / kv_heads;
     const bool single = (int64_t)p.max_len * group <= kTile;
     const int stride = single ? group : 1, dealt = !single && splits == 1;
-    const WinArgs a{p.lengths, p.tok_off, p.av_items, p.av_cap, p.status, keys.first, keys.len, keys.rows, keys.max_len, q, k, v, out,
-                    ldq, ldk, ldv, ldo, p.heads, group, group == 1 ? 0u : (uint32_t)(0xffffffffu / (uint32_t)group + 1), window, sinks, scale, p.total_tokens, splits, stride, dealt, ws,
-                    ws ? ws + (int64_t)splits * rows * kHeadDim : nullptr};
+    const uint32_t magic = group == 1 ? 0u : 0xffffffffu / (uint32_t)group + 1u;
+    const WinArgs a{p.lengths, p.tok_off, p.av_items, p.av_cap, p.status, keys.first, keys.len, keys.rows, keys.max_len, q, k, v,
+                    out, ldq, ldk, ldv, ldo, p.heads, group, magic, window, sinks, scale, p.total_tokens, splits, stride, dealt,
+                    ws, ws ? ws + (int64_t)splits * rows * kHeadDim : nullptr};
     // one workgroup per entry that a plan of this capacity can hold (in rows of 2^20)
     constexpr int64_t kUnit = 8 * kStreamRun, kRow = 1 << 20;
     int64_t g = std::max<int64_t>(p.av_cap / stride, 1);

@@ -102,7 +102,7 @@ def plan(**over):
 
 
 @pytest.mark.parametrize("over,status", [
-    (dict(plan=None), ARG), (dict(dtype=3), DTYPE), (dict(heads=0), ARG), (dict(heads=1 << 20), SHAPE), (dict(layout=4), ARG),
+    (dict(plan=None), ARG), (dict(dtype=3), DTYPE), (dict(heads=0), ARG), (dict(big=1), ARG), (dict(heads=1 << 20), SHAPE), (dict(layout=4), ARG),
     (dict(layout=-1), ARG), (dict(rot_dim=0), SHAPE), (dict(rot_dim=33), SHAPE), (dict(rot_dim=66), SHAPE),
     (dict(head_dim=514, ldx=9000, ldy=9000), SHAPE), (dict(amplitude=float("inf")), ARG), (dict(x=None), ARG),
     (dict(y=None), ARG), (dict(ldx=1023), SHAPE), (dict(ldy=1000), SHAPE), (dict(x=A + 1), SHAPE), (dict(inv_freq=None), ARG),
@@ -112,6 +112,9 @@ def plan(**over):
 def test_rotary_refuses(over, status):
     ok = dict(plan=plan(), x=A, ldx=1024, y=A + MB, ldy=1024, heads=16, head_dim=64, rot_dim=32, layout=0,
               inv_freq=A + 2 * MB, amplitude=1.0, pos_start=A + 3 * MB, dtype=BF16, stream=None)
+    over = dict(over)
+    if over.pop("big", 0):
+        over["plan"] = plan(total_tokens=2 ** 24 + 1)
     assert call("packed_rotary", ROTARY, ok, **over) == status
     assert call("packed_rotary", ROTARY, ok, plan=plan(total_tokens=0), x=None, y=None, inv_freq=None) == 0
 
@@ -190,7 +193,10 @@ def test_window_workspace():
     assert f(plan(), 128, 3, 100, 4, BF16, ctypes.byref(n)) == SHAPE
     assert f(plan(), 128, 2, -1, 4, BF16, ctypes.byref(n)) == ARG
     assert f(plan(), -1, 2, 1, 4, BF16, ctypes.byref(n)) == ARG
-    assert f(plan(total_tokens=2 ** 30, max_len=2 ** 12), 128, 2, 1, 4, BF16, ctypes.byref(n)) == SHAPE
+    assert f(plan(total_tokens=2 ** 24 + 1, max_len=2 ** 12), 128, 2, 1, 4, BF16, ctypes.byref(n)) == ARG
+    assert f(plan(), 2 ** 30 + 1, 2, 1, 4, BF16, ctypes.byref(n)) == ARG
+    assert f(plan(total_tokens=2 ** 24, max_len=2 ** 12, heads=256), 128, 1, 1, 4, BF16, ctypes.byref(n)) == SHAPE
+    assert f(plan(heads=32769), 128, 1, 1, 4, BF16, ctypes.byref(n)) == SHAPE
     assert f(plan(), 128, 2, 100, 4, 5, ctypes.byref(n)) == DTYPE
 
 

@@ -326,3 +326,19 @@ def test_replayed_graphs_and_two_calls_at_once(dtype):
         go(1, ref[1], wss[2], side)
         torch.cuda.synchronize()
         assert torch.equal(outs[0], ref[0]) and torch.equal(outs[1], ref[1])
+
+
+def test_windows_of_any_size():
+    # Python integers past 32 bits are open windows, not wrapped ones
+    import paper_2110_10221_amd as rag
+
+    L = [100, 30]
+    q, k, v = (P.normal(s, 130, 128).cuda() for s in range(3))
+    outs = []
+    for window, sinks in ((ALL, 0), (2 ** 31, 0), (2 ** 32 + 1, 0), (10 ** 15, 0), (3, 2 ** 32 + 1), (0, 10 ** 15)):
+        plan, out = make_plan(L, 2), torch.empty_like(q)
+        rag.ragged_attention_window(plan, q, k, v, out, 0.125, window, sinks)
+        outs.append(out)
+    assert all(torch.equal(o, outs[0]) for o in outs[1:4])
+    tol = 4 * 2.0 ** -8 * v.float().abs().max()  # the others' masks are the same, their chunks in another order
+    assert all((o.float() - outs[0].float()).abs().max() <= tol for o in outs[4:])
