@@ -280,6 +280,14 @@ def packed_layernorm(x, gamma, beta, y, eps=1e-5, stream=None):
 # single tokens takes as long as its host side, so the checks are one comparison each and
 # pointers go to ctypes as integers.
 
+class _Codes(dict):
+    def __missing__(self, dtype):
+        raise TypeError(f"unsupported tensor dtype {dtype} (bfloat16 or float32)")
+
+
+_CODES = _Codes({torch.float32: RAG_F32, torch.bfloat16: RAG_BF16})
+
+
 def _refuse(name, t, shape, dtype, dev):
     raise ValueError(f"{name} must be {list(shape)} of {dtype} on device {dev} with unit stride in its last dimension, "
                      f"not {list(t.shape)} of {t.dtype} on {t.device}, strides {list(t.stride())}")
@@ -327,17 +335,17 @@ def packed_rmsnorm(x, gamma, y=None, eps=1e-6, residual=None, x_out=None, q=None
     st = _c_rmsnorm(x.data_ptr(), _mat("x", x, shape, dt, dev), _addr(residual), _mat("residual", residual, shape, dt, dev),
                     _vec("gamma", gamma, d, dt, dev), eps, _addr(x_out), _mat("x_out", x_out, shape, dt, dev),
                     _addr(y), _mat("y", y, shape, dt, dev), _addr(q), _mat("q", q, shape, torch.int8, dev),
-                    _vec("q_scale", q_scale, T, torch.float32, dev), T, d, _dtype_code(x), _launch_stream(stream, dev))
+                    _vec("q_scale", q_scale, T, torch.float32, dev), T, d, _CODES[dt], _launch_stream(stream, dev))
     if st:
         _check("packed_rmsnorm", st)
 
 
 def packed_quantize_i8(x, q, scale, stream=None):
     """8-bit rows of x [T, d] (tokens, or a weight matrix): q int8 [T, d], scale float32 [T]."""
-    shape, dev = x.shape, x.get_device()
+    shape, dt, dev = x.shape, x.dtype, x.get_device()
     T, d = shape
-    st = _c_quantize_i8(x.data_ptr(), _mat("x", x, shape, x.dtype, dev), _addr(q), _mat("q", q, shape, torch.int8, dev),
-                        _vec("scale", scale, T, torch.float32, dev), T, d, _dtype_code(x), _launch_stream(stream, dev))
+    st = _c_quantize_i8(x.data_ptr(), _mat("x", x, shape, dt, dev), _addr(q), _mat("q", q, shape, torch.int8, dev),
+                        _vec("scale", scale, T, torch.float32, dev), T, d, _CODES[dt], _launch_stream(stream, dev))
     if st:
         _check("packed_quantize_i8", st)
 
@@ -353,7 +361,7 @@ def packed_linear_i8(x, x_scale, w, w_scale, y, bias=None, residual=None, act=RA
     st = _c_linear_i8(x.data_ptr(), _mat("x", x, (T, K), torch.int8, dev), _vec("x_scale", x_scale, T, torch.float32, dev),
                       w.data_ptr(), _vec("w_scale", w_scale, N, torch.float32, dev), _vec("bias", bias, N, dt, dev),
                       _addr(residual), _mat("residual", residual, (T, N), dt, dev), act, y.data_ptr(),
-                      _mat("y", y, (T, N), dt, dev), T, K, N, _dtype_code(y), _launch_stream(stream, dev))
+                      _mat("y", y, (T, N), dt, dev), T, K, N, _CODES[dt], _launch_stream(stream, dev))
     if st:
         _check("packed_linear_i8", st)
 
@@ -378,7 +386,7 @@ def packed_rotary(plan: Plan, x, y, inv_freq, heads, head_dim=RAG_HEAD_DIM, layo
     st = _c_rotary(plan.ref(), x.data_ptr(), _mat("x", x, shape, dt, dev), y.data_ptr(), _mat("y", y, shape, dt, dev), heads,
                    head_dim, 2 * n, layout | (RAG_ROTARY_INVERSE if inverse else 0),
                    _vec("inv_freq", inv_freq, n, torch.float64, dev), amplitude,
-                   _vec("pos_start", pos_start, plan.batch, torch.int32, dev), _dtype_code(x), _launch_stream(stream, dev, plan))
+                   _vec("pos_start", pos_start, plan.batch, torch.int32, dev), _CODES[dt], _launch_stream(stream, dev, plan))
     if st:
         _check("packed_rotary", st)
 
@@ -386,9 +394,9 @@ def packed_rotary(plan: Plan, x, y, inv_freq, heads, head_dim=RAG_HEAD_DIM, layo
 def ragged_attention_window_workspace(plan: Plan, max_kv_len, window, sinks=0, kv_heads=None, dtype=torch.bfloat16):
     """Workspace bytes of the two calls below (max_kv_len: plan.max_len for the first; may be 0)."""
     n = ctypes.c_size_t()
-    code = {torch.bfloat16: RAG_BF16, torch.float32: RAG_F32}.get(dtype, -1)
     _check("ragged_attention_window_workspace", _c_window_ws(plan.ref(), min(max_kv_len, _I32_MAX), kv_heads or plan.heads,
-                                                             min(window, _I32_MAX), min(sinks, _I32_MAX), code, ctypes.byref(n)))
+                                                             min(window, _I32_MAX), min(sinks, _I32_MAX), _CODES[dtype],
+                                                             ctypes.byref(n)))
     return n.value
 
 
@@ -398,10 +406,10 @@ def _window_operands(plan, q, k, v, out, kv_rows, kv_heads, head_dim, workspace)
     shape, kv = (plan.total_tokens, plan.heads * head_dim), (kv_rows, kv_heads * head_dim)
     lds = (_mat("q", q, shape, dt, dev), _mat("k", k, kv, dt, dev), _mat("v", v, kv, dt, dev), _mat("out", out, shape, dt, dev))
     if workspace is None:
-        return _dtype_code(q), dev, lds, None, 0
+        return _CODES[dt], dev, lds, None, 0
     if not workspace.is_contiguous() or workspace.get_device() != dev:
         raise ValueError("workspace must be contiguous and on the operands' device")
-    return _dtype_code(q), dev, lds, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return _CODES[dt], dev, lds, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def ragged_attention_window(plan: Plan, q, k, v, out, scale, window, sinks=0, kv_heads=None, head_dim=RAG_HEAD_DIM,
