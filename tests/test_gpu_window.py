@@ -342,3 +342,70 @@ def test_windows_of_any_size():
     assert all(torch.equal(o, outs[0]) for o in outs[1:4])
     tol = 4 * 2.0 ** -8 * v.float().abs().max()  # the others' masks are the same, their chunks in another order
     assert all((o.float() - outs[0].float()).abs().max() <= tol for o in outs[4:])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("L,heads,kv_heads", [([64, 1, 0, 63], 2, 2), ([16, 3, 0, 1, 15], 8, 2), ([1, 0, 1, 1], 64, 1),
+                                              ([1, 1, 1], 65, 1), ([8, 7, 0], 16, 2), ([4, 5], 16, 1)])
+def test_rows_that_fill_one_tile(dtype, L, heads, kv_heads):
+    # sequences whose rows of a key head are at most one tile (one entry in G launched), and just past it
+    packed(L, heads, kv_heads, 9, 2, dtype, seed=heads)
+    cached(L, [n + 37 * i for i, n in enumerate(L)], heads, kv_heads, 30, 2, dtype, seed=heads)
+
+
+def test_many_sequences():
+    rng = np.random.default_rng(5)
+    cached([1] * 300, rng.integers(1, 90, 300).tolist(), 4, 2, 33, 4, "bf16", seed=1)
+    packed(rng.integers(0, 40, 300).tolist(), 2, 1, 11, 1, "bf16", seed=2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_loose_bounds(dtype):
+    # max_kv_len and the plan's max_len far above every length: splits without a chunk, entries without rows
+    import paper_2110_10221_amd as rag
+
+    n, _ = cached([1, 1], [40, 300], 4, 2, ALL, 0, dtype, seed=3, max_kv=100000)
+    assert n > 0
+    n, _ = cached([1, 2], [1, 2], 2, 1, 50000, 1, dtype, seed=3, max_kv=100000)
+    assert n > 0
+    L, T = [50, 3], 53
+    plan = rag.Plan(torch.tensor(L, dtype=torch.int32).cuda(), T, 4000, 2)
+    rag.ragged_offsets(plan)
+    q, k, v = (P.normal(s, T, 128, dtype=dtype) for s in range(3))
+    out = torch.empty(T, 128, dtype=q.dtype, device="cuda")
+    ws = torch.empty(rag.ragged_attention_window_workspace(plan, 4000, ALL, 0, None, q.dtype), dtype=torch.uint8, device="cuda")
+    rag.ragged_attention_window(plan, q.cuda(), k.cuda(), v.cuda(), out, 0.125, ALL, 0, workspace=ws)
+    check(out, dtype, L, 2, 2, q, k, v, [0, 50], L, ALL, 0, 0.125)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_query_that_is_not_finite_stays_alone(dtype, bad):
+    import paper_2110_10221_amd as rag
+
+    L, H = [100, 30], 4
+    q, k, v = P.normal(1, 130, H * 64, dtype=dtype), P.normal(2, 130, 128, dtype=dtype), P.normal(3, 130, 128, dtype=dtype)
+    dirty = q.clone()
+    dirty[50, 64 * 2 + 5] = bad  # token 50, head 2
+    plan, out = make_plan(L, H), torch.empty(130, H * 64, dtype=q.dtype, device="cuda")
+    rag.ragged_attention_window(plan, dirty.cuda(), k.cuda(), v.cuda(), out, 0.125, 40, 2, 2)
+    ref, mag, bound, count = P.window_attention(L, H, 2, q, k, v, [0, 100], L, 40, 2, 0.125)
+    ok = ((out.cpu().double() - ref).abs() <= P.window_tolerance(dtype, ref, mag, bound, count)).reshape(130, H, 64)
+    rest = torch.ones(130, H, dtype=torch.bool)
+    rest[50, 2] = False
+    assert ok[rest].all()
+    assert torch.isnan(out.cpu().reshape(130, H, 64)[50, 2].float()).all()
+
+
+def test_a_range_outside_the_cache_with_split_keys():
+    import paper_2110_10221_amd as rag
+
+    plan = make_plan([1, 1], 2)
+    q, k = torch.zeros(2, 128, device="cuda"), torch.zeros(4000, 128, device="cuda")
+    n = rag.ragged_attention_window_workspace(plan, 4000, ALL, 0, None, torch.float32)
+    assert n > 0
+    out = torch.full_like(q, 7.0)
+    rag.ragged_attention_window_cached(plan, q, k, k, torch.tensor([0, 3000]).cuda(),
+                                       torch.tensor([4000, 1001], dtype=torch.int32).cuda(), 4000, out, 1.0, ALL,
+                                       workspace=torch.empty(n, dtype=torch.uint8, device="cuda"))
+    assert plan.data_errors() == ["keys outside the cache"] and (out == 7.0).all()
