@@ -64,6 +64,22 @@ __device__ __forceinline__ void barrier_seen() {
     asm volatile("" ::: "memory");
 }
 
+// GELU's tanh form for bf16 outputs: x (1 + tanh u) / 2 = x / (1 + exp(-2u)), the hardware's power of two and
+// reciprocal within two steps of fp32 (tanhf is six times the instructions: 35475 x 1024 x 4096
+// 304 us with it, 214 without).
+__device__ __forceinline__ float gelu_tanh_fast(float x) {
+    constexpr float k = 2.0f * 0.79788456080286536f * 1.4426950408889634f;  // 2 sqrt(2 / pi) log2(e)
+    const float u = x * fmaf(x * x, k * 0.044715f, k);
+    return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-u));
+}
+
+template <bool BF16, int ACT>
+__device__ __forceinline__ float finish_act(float x) {
+    if constexpr (BF16 && ACT == 2) return gelu_tanh_fast(x);
+    else if constexpr (BF16) return activate_bf16<ACT>(x);
+    else return activate<ACT>(x);
+}
+
 // Eight consecutive features of one token, from sums to the stored row.
 template <bool BF16, int ACT>
 struct Finish {
@@ -100,7 +116,7 @@ struct Finish {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float z = fmaf((float)sum[e] * xs, ws[e >> 2][e & 3], bv[e]);
-            v[e] = BF16 ? activate_bf16<ACT>(z) : activate<ACT>(z);
+            v[e] = finish_act<BF16, ACT>(z);
         }
         if (residual) {
 #pragma unroll
@@ -445,9 +461,9 @@ hipError_t launch_type(const I8Args& a, int act, hipStream_t s) {
 // nk the 128-k steps, rounds the tiles of the busiest CU, `alone` a step's latency and `step` its
 // share of a busy CU's time, the epilogue longer with an activation or fp32 outputs.  Fitted to
 // 205 shapes (T 17 to 40000, K 256 to 8192, N 64 to 8192, both types, every epilogue), where
-// the choice takes 2% more than the fastest form on average and 23% at worst.  Both sides, us on forms 1
-// to 5: 2237 x 2048 x 512 fp32 9.6, 8.9, 9.1, 14.7, 12.2; 35475 x 1024 x 4096 GELU 395, 291, 264, 225,
-// 229; 35475 x 4096 x 1024 with residual 336, 225, 190, 168, 140.
+// the choice takes 2% more than the fastest form on average and 23% at worst (1.3% and 21% on 355
+// others).  Both sides, us on forms 1 to 5: 2237 x 2048 x 512 fp32 9.6, 8.9, 9.1, 14.7, 12.2;
+// 35475 x 1024 x 4096 GELU 395, 291, 264, 225, 229; 35475 x 4096 x 1024 with residual 336, 225, 190, 168, 140.
 int linear_form_i8(int64_t T, int64_t K, int64_t N, int act, bool bf16, int64_t cus) {
     if (T <= 16) return 0;
     struct Cost {
