@@ -5,11 +5,14 @@
 // One pass over the keys that some row of an item sees, like the fused ragged attention
 // (attention.hip): chunks of 32 keys through two LDS stages, S^T = K Q^T in fp32, a running
 // reference m and sum of the softmax, O^T += V^T E^T, one division at the end.
-//   items   the entries of the plan's Attn.V list, 64 rows per workgroup of two waves.  A
+//   items   the entries of the plan's Attn.V list, 64 rows per workgroup of two waves (or
+//           two entries, 128 rows and four waves).  A
 //           row is a (token, query head) pair: the G heads that share a key head
 //           are consecutive rows, so their keys are read once and a step of
 //           single tokens fills rows with heads.  Entry (b, h, ti) is tile (h % G) *
-//           ceil(L_b / 64) + ti of key head h / G; tiles past the last row return.
+//           ceil(L_b / 64) + ti of key head h / G, from its last tile to its first (those that see
+//           most start first: two sequences of 8192 tokens, all visible, 500 us, 491 so);
+//           entries past them return.
 //   chunks  of a tile: those of the window from the last to the first, then the sinks'.
 //           Downwards because a row's own key is always visible: the first chunk then
 //           sets nearly every row's reference, where upwards the rows whose
@@ -18,16 +21,17 @@
 //           skipped by it.  Hidden values are multiplied by a zero, so those that are not
 //           finite are taken out of such a chunk's operand and added to the rows that see
 //           them after the last chunk (in the loop their handling cost 35 registers, the
-//           fourth wave per SIMD: six prompts of 1500 to 8192 tokens 172 us, 161 without).
+//           fourth wave per SIMD: six prompts of 1500 to 8192 tokens 172 us, 161 without, when
+//           it was moved).  The masks are bits of a word per row and chunk (166 us, 161).
 //   splits  where few rows meet many keys the chunks are dealt to several workgroups
 //           (blockIdx.y), whose (reference, sum, output) states a second launch joins.
 // bf16 rounds the unnormalised exponentials to bf16 for the P V product (a relative 2^-8 at most
 // of each of many terms, beside 2^-8 of the stored result) and nothing else; fp32
 // products run on v_mfma_f32_32x32x2f32 and round nothing.
-// What bounds it: for prompts the exponentials and the vector work around them (16 v_exp_f32
-// of 16 cycles a chunk and wave, about 420 cycles with the sums and conversions, beside 256 of
-// MFMAs that pass under another wave's: six prompts of 1500 to 8192 tokens, window 1024, 16/4 heads, 159 us,
-// 640 TFLOP/s), in fp32 the 4096 MFMA cycles of a chunk; for single tokens the bytes of K and V: 32
+// What bounds it: for prompts the vector work of the softmax, about 420 cycles of a chunk and wave beside
+// 256 of MFMAs that pass under another wave's, and the copies into LDS (six prompts of 1500 to 8192
+// tokens, window 1024, 16/4 heads: 149 us, 690 TFLOP/s; timed without its exponentials 8% less, without its copies
+// 14%, without half of its MFMAs 3%), in fp32 the 4096 MFMA cycles of a chunk; for single tokens the bytes of K and V: 32
 // tokens over 4100 keys of 4 heads each, 134 MB, 28 us (4.8 TB/s; a large copy reaches 5.2) and 4.8 for
 // the join.
 #include <algorithm>
@@ -41,7 +45,6 @@ namespace rag {
 namespace {
 
 constexpr int kWinBlock = 32;       // rows per wave
-constexpr int kWinWaves = kTile / kWinBlock, kWinThreads = kWinWaves * kWave;
 constexpr int kWinChunk = 32;       // keys per LDS stage
 
 struct WinArgs {
@@ -62,7 +65,7 @@ struct WinArgs {
     int window, sinks;
     float scale;
     int T, splits;
-    int stride;      // between the list entries that hold rows: G where no sequence has more than one tile a key head
+    int stride;      // between the list entries that hold rows: G where no sequence has more than one tile a key head, 2 of 128-row tiles
     int dealt;       // entries go to the XCDs in runs (else one by one)
     float* part_o;   // [splits][T][heads][64] unnormalised outputs
     float* part_ml;  // [splits][T][heads][2] reference and sum
@@ -108,14 +111,15 @@ __device__ __forceinline__ void copy_1k(__amdgpu_buffer_rsrc_t r, void* dst, int
 
 __device__ __forceinline__ bool finite_f32(float v) { return fabsf(v) <= FLT_MAX; }
 
-template <bool BF16>
-__global__ __launch_bounds__(kWinThreads, BF16 ? 4 : 2)
+template <bool BF16, int NW>
+__global__ __launch_bounds__(NW * kWave, BF16 ? 4 : 2)
 void k_attention_window(WinArgs a) {
     using W = WinT<BF16>;
     using T = typename W::T;
+    constexpr int kRows = NW * kWinBlock;                  // rows of a tile
     constexpr int kStage = 2 * kWinChunk * W::kRow;        // K rows, then V rows
     constexpr int kBlockRows = 1024 / W::kRow;             // rows of a 1 KB copy
-    constexpr int kBlocks = kWinChunk / kBlockRows / kWinWaves;  // copies of K (and of V) per wave and chunk
+    constexpr int kBlocks = kWinChunk / kBlockRows / NW;  // copies of K (and of V) per wave and chunk
     constexpr int kEs = (int)sizeof(T);
     __shared__ __attribute__((aligned(16))) uint8_t kvs[2 * kStage];
     const int wave = uni(threadIdx.x / kWave), lane = threadIdx.x % kWave;
@@ -146,8 +150,9 @@ void k_attention_window(WinArgs a) {
     const int L = uni(len), t0 = uni(off);
     const auto per_group = [&](int x) { return G == 1 ? x : (int)__umulhi((uint32_t)x, a.magic); };  // x / G, x < 2^16
     const int hk = uni(per_group(h)), rows = L * G;
-    const int r0 = ((h - hk * G) * ((L + kTile - 1) / kTile) + ti) * kTile;
-    if (r0 >= rows) return;
+    const int entry_no = (h - hk * G) * ((L + kTile - 1) / kTile) + ti;  // of the sequence and key head
+    const int r0 = ((rows - 1) / kRows - entry_no / (kRows / kTile)) * kRows;
+    if (r0 < 0) return;
     const int n = uni(kvn);  // keys
     const int64_t first = uni64(kv0);
     if (a.kv_len) {
@@ -160,7 +165,7 @@ void k_attention_window(WinArgs a) {
     // the tile's positions
     const int tok0 = uni(G == 1 ? r0 : r0 / G), rem = r0 - tok0 * G;  // the tile's first row
     const auto token = [&](int row) { return min(tok0 + per_group(rem + row), L - 1); };  // of a row of the tile
-    const int tlo = past + tok0, thi = past + uni(token(kTile - 1));
+    const int tlo = past + tok0, thi = past + uni(token(kRows - 1));
     // chunks: window [cw0, cw1) downwards, then the sinks' [0, cs) below them
     int cw0 = (window_below(tlo, a.window) + 1) / kWinChunk, cw1 = thi / kWinChunk + 1;
     if (thi < 0 || a.window == 0) cw0 = cw1 = INT32_MAX / kWinChunk;
@@ -220,7 +225,7 @@ void k_attention_window(WinArgs a) {
         if (flip) qf[u] ^= BF16 ? 0x80008000u : 0x80000000u;
     }
     float m = -FLT_MAX, lsum = 0.f;
-    bool fresh = true;  // no chunk yet
+    int fresh = 1;  // no chunk yet (a bool would be a lane mask)
     bool infinite = false;  // a chunk with hidden keys held values that are not finite
     floatx16 oacc[2];
 #pragma unroll
@@ -260,8 +265,14 @@ void k_attention_window(WinArgs a) {
         };
         const auto hide = [&] {
             if (!whole) {
+                // bit j: key c0 + 4 h2 + j is seen
+                const auto below = [](int n) { return n >= 32 ? ~0u : ~(~0u << max(n, 0)); };
+                const uint32_t seen = ((below(p + 1 - c0) & ~below(from - c0)) | below(sink_range - c0)) >> (4 * h2);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[r] = sees(c0 + 4 * h2 + 8 * (r / 4) + (r % 4)) ? acc[r] : -INFINITY;
+                for (int r = 0; r < 16; ++r) {
+                    const uint32_t all = (uint32_t)__builtin_amdgcn_sbfe((int)seen, 8 * (r / 4) + r % 4, 1);  // or no bits
+                    acc[r] = __uint_as_float((all & __float_as_uint(acc[r])) | (~all & 0xff800000u));
+                }
             }
         };
         const auto chunk_max = [&] {
@@ -305,6 +316,7 @@ void k_attention_window(WinArgs a) {
                 : "memory");
         }
         hide();
+        fresh = uni(fresh);
         if (fresh) m = fmaxf(chunk_max(), -FLT_MAX);  // (no visible key: any later score is far above)
         float ps = exps();
         // a lane sum above kSumCap (or NaN) means a score well above m: raise m to the
@@ -322,17 +334,18 @@ void k_attention_window(WinArgs a) {
             m = mn;
             ps = exps();
         }
-        fresh = false;
+        fresh = 0;
         lsum += ps;
         // Values that are not finite, among hidden keys, would reach every row (0 times infinity): they
         // are taken out of the operand here and added after the last chunk.
         if constexpr (BF16) {
             if (!whole) {
-                uint32_t bad = 0;  // an exponent of all ones in either half
+                typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+                u16x2 top = {0, 0};  // largest exponents: all ones if not finite
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    bad |= ((tr[e >> 3][e >> 2 & 1][e >> 1 & 1][e & 1] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-                if (__ballot(bad != 0) != 0) {
+                    top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, tr[e >> 3][e >> 2 & 1][e >> 1 & 1][e & 1] & 0x7f807f80u));
+                if (__ballot(max(top[0], top[1]) == 0x7f80) != 0) {
                     infinite = true;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
@@ -343,6 +356,7 @@ void k_attention_window(WinArgs a) {
                     }
                 }
             }
+            __builtin_amdgcn_s_setprio(1);  // (matrix instructions of one wave beside the others' vector work)
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 u32x4 pw;
@@ -353,6 +367,7 @@ void k_attention_window(WinArgs a) {
                     oacc[cb] = mfma32x32x16(as_bf16x8(u32x4{tr[t][cb][0][0], tr[t][cb][0][1], tr[t][cb][1][0], tr[t][cb][1][1]}),
                                             as_bf16x8(pw), oacc[cb]);
             }
+            __builtin_amdgcn_s_setprio(0);
         } else {
             // the lane's keys 8 (r / 4) + 4 h2 + r % 4 of channel 32 cb + l32
             float vf[2][16];
@@ -389,7 +404,7 @@ void k_attention_window(WinArgs a) {
     const auto step = [&](int i, auto stg) {
         constexpr int stage = decltype(stg)::value;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's copies of chunk i
-        attn_barrier();  // ... and the other wave's; the other stage was last read in step i - 1
+        attn_barrier();  // ... and the other waves'; the other stage was last read in step i - 1
         if (i + 1 < i1) issue(i + 1, stage ^ kStage);
         const int c = chunk(i);
         if (c > last || (c < wfirst && c >= sinks1)) return;  // no row of the wave sees a key of it
@@ -566,7 +581,14 @@ hipError_t launch_attention_window(const PlanView& p, int dtype, const void* q, 
     // to the XCDs in turn (in runs, eight heads' splits would all be one XCD's).
     const int group = p.heads / kv_heads;
     const bool single = (int64_t)p.max_len * group <= kTile;
-    const int stride = single ? group : 1, dealt = !single && splits == 1;
+    // Tiles of 128 rows, whose four waves share a chunk's copies, in bf16 from groups of four on (their
+    // positions span at most a chunk, else the waves wait for each other's first and last ones), where two entries
+    // of a key head always make one (an odd group's would leave workgroups empty).  Us on 64 and 128
+    // rows: six prompts of 1500 to 8192 tokens, 16/4 heads, window 1024 163, 156; 128 sequences to 512
+    // tokens, 16/4 heads, window 128 55.5, 54.1; 256 of 17 tokens 16.1, 12.4; groups of two, 16 of 300
+    // tokens, 8/4 heads 10.3, 11.2; two of 8192, 16/8 heads 430, 442.  fp32, bound by its MFMAs: equal.
+    const bool wide = dtype == 1 && !single && splits == 1 && group >= 4 && group % 2 == 0;
+    const int stride = single ? group : wide ? 2 : 1, dealt = !single && splits == 1;
     const uint32_t magic = group == 1 ? 0u : 0xffffffffu / (uint32_t)group + 1u;
     const WinArgs a{p.lengths, p.tok_off, p.av_items, p.av_cap, p.status, keys.first, keys.len, keys.rows, keys.max_len, q, k, v,
                     out, ldq, ldk, ldv, ldo, p.heads, group, magic, window, sinks, scale, p.total_tokens, splits, stride, dealt,
@@ -576,8 +598,8 @@ hipError_t launch_attention_window(const PlanView& p, int dtype, const void* q, 
     int64_t g = std::max<int64_t>(p.av_cap / stride, 1);
     if (dealt) g = (g + kUnit - 1) / kUnit * kUnit;  // dealing is a permutation of these
     const dim3 grid((unsigned)std::min(g, kRow), (unsigned)splits, (unsigned)((g + kRow - 1) / kRow));
-    auto* f = dtype == 1 ? &k_attention_window<true> : &k_attention_window<false>;
-    hipLaunchKernelGGL(f, grid, dim3(kWinThreads), 0, s, a);
+    auto* f = wide ? &k_attention_window<true, 4> : dtype == 1 ? &k_attention_window<true, 2> : &k_attention_window<false, 2>;
+    hipLaunchKernelGGL(f, grid, dim3((wide ? 4 : 2) * kWave), 0, s, a);
     if (splits > 1) {
         if (dtype == 1) launch_join<true>(a, splits, rows, s);
         else launch_join<false>(a, splits, rows, s);

@@ -409,3 +409,39 @@ def test_a_range_outside_the_cache_with_split_keys():
                                        torch.tensor([4000, 1001], dtype=torch.int32).cuda(), 4000, out, 1.0, ALL,
                                        workspace=torch.empty(n, dtype=torch.uint8, device="cuda"))
     assert plan.data_errors() == ["keys outside the cache"] and (out == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,kv_heads", [(4, 1), (8, 2), (12, 2), (16, 2), (10, 2)])
+@pytest.mark.parametrize("window,sinks", [(45, 3), (ALL, 0)])
+def test_groups_of_heads_over_several_tiles(dtype, heads, kv_heads, window, sinks):
+    # rows of a key head one below, at and past multiples of 64 and 128, empty and single sequences between
+    L = [1, 0, 31, 32, 33, 130, 16, 17, 64, 0, 65]
+    packed(L, heads, kv_heads, window, sinks, dtype, seed=heads, pad=8)
+    cached(L, [n + 29 * (i % 3) for i, n in enumerate(L)], heads, kv_heads, window, sinks, dtype, seed=heads + 1)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_hidden_values_in_groups_of_four(bad):
+    import paper_2110_10221_amd as rag
+
+    L, H, KV, window, sinks = [150, 70], 8, 2, 40, 3
+    q, k, v = P.normal(31, 220, H * 64), P.normal(32, 220, KV * 64), P.normal(33, 220, KV * 64)
+    spots = [(0, 1), (0, 60), (0, 149), (1, 33)]
+    dirty = v.clone()
+    for b, j in spots:
+        dirty[(0, 150)[b] + j, 3::9] = bad
+    plan, out = make_plan(L, H), torch.empty(220, H * 64, dtype=q.dtype, device="cuda")
+    rag.ragged_attention_window(plan, q.cuda(), k.cuda(), dirty.cuda(), out, 0.125, window, sinks, KV)
+    ref, mag, bound, count = P.window_attention(L, H, KV, q, k, v, [0, 150], L, window, sinks, 0.125)
+    ok = (out.cpu().double() - ref).abs() <= P.window_tolerance("bf16", ref, mag, bound, count)
+    sees = torch.zeros(220, dtype=torch.bool)
+    for b, j in spots:
+        for i in range(j, L[b]):
+            if j > i - window or j < sinks:
+                sees[(0, 150)[b] + i] = True
+    cols = torch.zeros(KV, 64, dtype=torch.bool)
+    cols.view(-1)[3::9] = True
+    cols = cols.repeat_interleave(H // KV, 0).reshape(-1)  # a query head's channels are its key head's
+    assert ok[~sees].all() and ok[sees][:, ~cols].all()
+    assert not torch.isfinite(out.cpu().float()[sees][:, cols]).any()
