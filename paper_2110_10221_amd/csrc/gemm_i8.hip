@@ -190,8 +190,9 @@ __device__ __forceinline__ void i8_tile(const I8Args& a, int m0, int n0, int8_t*
     // are waited for and its first group read, and the copies of step k + ST go out
     // between the MFMAs into the stage every wave has now read.  (Group g of step k sits in
     // slot (k * G + g) % 2: with one group per step the slots alternate by step.)
-    auto step = [&](int k, auto last, auto par) {
-        constexpr bool kLast = decltype(last)::value;
+    // `kind` 2: such a step; 1: one of the last ST, with no copies left; 0: the last.
+    auto step = [&](int k, auto kind, auto par) {
+        constexpr int kKind = decltype(kind)::value;
         constexpr int kPar = decltype(par)::value;
         int8_t* const next = st + C::kStage == sm + ST * C::kStage ? sm : st + C::kStage;
 #pragma unroll
@@ -199,9 +200,9 @@ __device__ __forceinline__ void i8_tile(const I8Args& a, int m0, int n0, int8_t*
             const int slot = (kPar * G + g) % 2;
             if (g + 1 < G) {
                 read(1 - slot, st, g + 1);
-            } else if constexpr (!kLast) {
+            } else if constexpr (kKind > 0) {
                 __builtin_amdgcn_sched_barrier(0);  // the MFMAs before go out ahead of the wait
-                wait_vm<(ST - 2) * NC>();
+                wait_vm<kKind == 2 ? (ST - 2) * NC : 0>();
                 barrier_seen();
                 read(1 - slot, next, 0);
             }
@@ -212,7 +213,7 @@ __device__ __forceinline__ void i8_tile(const I8Args& a, int m0, int n0, int8_t*
 #pragma unroll
                 for (int j = 0; j < FM; ++j) {
                     acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[slot][i], fb[slot][j], acc[i][j], 0, 0, 0);
-                    if constexpr (!kLast) {
+                    if constexpr (kKind == 2) {
 #pragma unroll
                         for (int c = 0; c < NC; ++c)
                             if (g + 1 == G && c * FM * FN / NC == i * FM + j) issue_one(k + ST, st, c);
@@ -234,22 +235,26 @@ __device__ __forceinline__ void i8_tile(const I8Args& a, int m0, int n0, int8_t*
         const int row = r0 + it * kRowStep;
         return m0 + (row / kPart) * (TM / C::WM) + s * kPart + row % kPart;
     };
-    constexpr std::integral_constant<int, 0> even{};
-    constexpr std::integral_constant<int, 1> odd{};
+    constexpr std::integral_constant<int, 0> even{}, last{};
+    constexpr std::integral_constant<int, 1> odd{}, rest{};
+    constexpr std::integral_constant<int, 2> copying{};
     int k = 0;
     if constexpr (G % 2 == 0) {
-        for (; k + 1 < nk; ++k) step(k, std::false_type{}, even);
-        step(k, std::true_type{}, even);
+        // (35475 x 1024 x 1024 with residual on 64 x 64 tiles 69 us, 73 with copies past the reduction)
+        for (; k + ST < nk; ++k) step(k, copying, even);
+        for (; k + 1 < nk; ++k) step(k, rest, even);
+        step(k, last, even);
     } else {
+        // (copies past the reduction, which store zeros: a test for them in the loop cost more at K = 4096, 8.4 us and 9.2)
         for (; k + 2 < nk; k += 2) {
-            step(k, std::false_type{}, even);
-            step(k + 1, std::false_type{}, odd);
+            step(k, copying, even);
+            step(k + 1, copying, odd);
         }
         if (k + 1 < nk) {
-            step(k, std::false_type{}, even);
-            step(k + 1, std::true_type{}, odd);
+            step(k, copying, even);
+            step(k + 1, last, odd);
         } else {
-            step(k, std::true_type{}, even);
+            step(k, last, even);
         }
     }
     wait_vm<0>();  // the copies past the reduction have landed: LDS is free
@@ -437,7 +442,7 @@ hipError_t launch_form(const I8Args& a, hipStream_t s) {
         case 1: return launch_tiles<I8Cfg<32, 64, 1, 2, 2, 4>, BF16, ACT>(a, s);
         case 2: return launch_tiles<I8Cfg<64, 64, 2, 2, 1, 3>, BF16, ACT>(a, s);
         case 3: return launch_tiles<I8Cfg<64, 128, 2, 2, 1, 3>, BF16, ACT>(a, s);
-        case 4: return launch_tiles<I8Cfg<128, 128, 2, 2, 1, 2>, BF16, ACT>(a, s);
+        case 4: return launch_tiles<I8Cfg<128, 128, 2, 4, 1, 2>, BF16, ACT>(a, s);
         default: return launch_big<BF16, ACT>(a, cus, s);
     }
 }
@@ -460,28 +465,29 @@ hipError_t launch_type(const I8Args& a, int act, hipStream_t s) {
 //     start + max(epilogue + nk * alone, rounds * (epilogue + nk * step))
 // nk the 128-k steps, rounds the tiles of the busiest CU, `alone` a step's latency and `step` its
 // share of a busy CU's time, the epilogue longer with an activation or fp32 outputs.  Fitted to
-// 205 shapes (T 17 to 40000, K 256 to 8192, N 64 to 8192, both types, every epilogue), where
-// the choice takes 2% more than the fastest form on average and 23% at worst (1.3% and 21% on 355
-// others).  Both sides, us on forms 1 to 5: 2237 x 2048 x 512 fp32 9.6, 8.9, 9.1, 14.7, 12.2;
+// 355 shapes (T 17 to 40000, K 256 to 8192, N 64 to 8192, both types, every epilogue), where
+// the choice takes 1.4% more than the fastest form on average and 28% at worst (1.1% and 29% on 355
+// others).  Both sides, us on forms 1 to 5: 2237 x 2048 x 512 fp32 10.6, 10.1, 10.4, 15.3, 13.0;
 // 35475 x 1024 x 4096 GELU 395, 291, 264, 225, 229; 35475 x 4096 x 1024 with residual 336, 225, 190, 168, 140.
 int linear_form_i8(int64_t T, int64_t K, int64_t N, int act, bool bf16, int64_t cus) {
     if (T <= 16) return 0;
     struct Cost {
         int tm, tn;
-        double start, epilogue, step, alone, act, f32;
+        double start, epilogue, step, alone, act, f32, act32;  // act: of bf16 outputs, act32 of fp32's
     };
-    static const Cost kForms[4] = {{32, 64, 2.37, 0.46, 0.148, 0.166, 0.24, 0.20}, {64, 64, 2.43, 0.49, 0.219, 0.254, 0.57, 0.48},
-                                   {64, 128, 2.24, 1.18, 0.336, 0.365, 1.43, 0.86}, {128, 128, 1.19, 2.08, 0.522, 0.727, 2.82, 1.74}};
+    static const Cost kForms[4] = {{32, 64, 2.32, 0.42, 0.158, 0.164, 0.05, 0.23, 0.31}, {64, 64, 2.38, 0.38, 0.237, 0.253, 0.14, 0.33, 0.76},
+                                   {64, 128, 2.35, 0.99, 0.361, 0.361, 0.34, 0.60, 2.15}, {128, 128, 0.63, 1.98, 0.541, 0.705, 0.83, 1.05, 3.8}};
     const auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
-    const double nk = (double)up(K, 128), a = act != 0, f = !bf16;
+    const double nk = (double)up(K, 128);
+    const auto extra = [&](double a, double f, double a32) { return (bf16 ? 0.0 : f) + (!act ? 0.0 : bf16 ? a : a32); };
     // 256 x 256: rounds of whole tiles, then one of quarters
     const int64_t big = up(T, 256) * up(N, 256), whole = i8_whole_tiles(big, cus);
-    const double extra = a * 9.05 + f * 5.68;
-    double best = up(whole, cus) * (10.53 + extra + nk * 1.486) + up(4 * (big - whole), cus) * (3.96 + extra / 4 + nk * 0.492);
+    const double x = extra(4.96, 4.99, 14.4);
+    double best = up(whole, cus) * (10.2 + x + nk * 1.57) + up(4 * (big - whole), cus) * (3.65 + x / 4 + nk * 0.485);
     int form = 5;
     for (int i = 0; i < 4; ++i) {
         const Cost& c = kForms[i];
-        const double e = c.epilogue + a * c.act + f * c.f32;
+        const double e = c.epilogue + extra(c.act, c.f32, c.act32);
         const int64_t rounds = up(up(T, c.tm) * up(N, c.tn), cus);
         const double t = c.start + std::max(e + nk * c.alone, rounds * (e + nk * c.step));
         if (t < best) best = t, form = i + 1;
