@@ -466,7 +466,7 @@ hipError_t launch_type(const I8Args& a, int act, hipStream_t s) {
 // nk the 128-k steps, rounds the tiles of the busiest CU, `alone` a step's latency and `step` its
 // share of a busy CU's time, the epilogue longer with an activation or fp32 outputs.  Fitted to
 // 355 shapes (T 17 to 40000, K 256 to 8192, N 64 to 8192, both types, every epilogue), where
-// the choice takes 1.4% more than the fastest form on average and 28% at worst (1.1% and 29% on 355
+// the choice takes 1.3% more than the fastest form on average and 30% at worst (0.9% and 29% on 355
 // others).  Both sides, us on forms 1 to 5: 2237 x 2048 x 512 fp32 10.6, 10.1, 10.4, 15.3, 13.0;
 // 35475 x 1024 x 4096 GELU 395, 291, 264, 225, 229; 35475 x 4096 x 1024 with residual 336, 225, 190, 168, 140.
 int linear_form_i8(int64_t T, int64_t K, int64_t N, int act, bool bf16, int64_t cus) {
@@ -476,14 +476,14 @@ int linear_form_i8(int64_t T, int64_t K, int64_t N, int act, bool bf16, int64_t 
         double start, epilogue, step, alone, act, f32, act32;  // act: of bf16 outputs, act32 of fp32's
     };
     static const Cost kForms[4] = {{32, 64, 2.32, 0.42, 0.158, 0.164, 0.05, 0.23, 0.31}, {64, 64, 2.38, 0.38, 0.237, 0.253, 0.14, 0.33, 0.76},
-                                   {64, 128, 2.35, 0.99, 0.361, 0.361, 0.34, 0.60, 2.15}, {128, 128, 0.63, 1.98, 0.541, 0.705, 0.83, 1.05, 3.8}};
+                                   {64, 128, 2.35, 0.99, 0.361, 0.361, 0.34, 0.60, 2.15}, {128, 128, 0.63, 1.98, 0.530, 0.705, 0.83, 1.05, 4.4}};
     const auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
     const double nk = (double)up(K, 128);
     const auto extra = [&](double a, double f, double a32) { return (bf16 ? 0.0 : f) + (!act ? 0.0 : bf16 ? a : a32); };
     // 256 x 256: rounds of whole tiles, then one of quarters
     const int64_t big = up(T, 256) * up(N, 256), whole = i8_whole_tiles(big, cus);
     const double x = extra(4.96, 4.99, 14.4);
-    double best = up(whole, cus) * (10.2 + x + nk * 1.57) + up(4 * (big - whole), cus) * (3.65 + x / 4 + nk * 0.485);
+    double best = up(whole, cus) * (10.2 + x + nk * 1.57) + up(4 * (big - whole), cus) * (4.05 + x / 4 + nk * 0.485);
     int form = 5;
     for (int i = 0; i < 4; ++i) {
         const Cost& c = kForms[i];
