@@ -27,10 +27,13 @@
 //           (blockIdx.y), whose (reference, sum, output) states a second launch joins.
 // bf16 rounds the unnormalised exponentials to bf16 for the P V product (a relative 2^-8 at most
 // of each of many terms, beside 2^-8 of the stored result) and nothing else; fp32
-// products run on v_mfma_f32_32x32x2f32 and round nothing.
+// products round nothing; they run on v_mfma_f32_16x16x4f32, 16 keys (4 for P V) by 16 rows at a time, and only
+// those that any row sees: a window of 96 is 111 keys to 16 rows, to 32 x 32 blocks it was 160 (batch 32 of
+// 16 to 512 tokens, 8 heads: 50.9 us on those, 46.5; 64 single tokens, caches to 2048, 8 heads 87, 79; six prompts
+// of 1500 to 8192 tokens, window 1024 933, 948).
 // What bounds it: for prompts the vector work of the softmax, about 420 cycles of a chunk and wave beside
 // 256 of MFMAs that pass under another wave's, and the copies into LDS (six prompts of 1500 to 8192
-// tokens, window 1024, 16/4 heads: 149 us, 690 TFLOP/s; timed without its exponentials 8% less, without its copies
+// tokens, window 1024, 16/4 heads: 147 us, 700 TFLOP/s; timed without its exponentials 8% less, without its copies
 // 14%, without half of its MFMAs 3%), in fp32 the 4096 MFMA cycles of a chunk; for single tokens the bytes of K and V: 32
 // tokens over 4100 keys of 4 heads each, 134 MB, 28 us (4.8 TB/s; a large copy reaches 5.2) and 4.8 for
 // the join.
@@ -83,7 +86,8 @@ template <>
 struct WinT<false> {
     using T = float;
     static constexpr int kRow = 256, kChunks = 16;
-    static __device__ __forceinline__ int swz(int row) { return row & 15; }
+    // (16 rows in any order, and rows q apart by 64 bytes: K fragments and V columns meet all banks)
+    static __device__ __forceinline__ int swz(int row) { return (row & 3) << 2 | (row >> 2 & 3); }
 };
 
 // Entry of a workgroup where neighbours go to one XCD in runs of kStreamRun.
@@ -97,8 +101,8 @@ __device__ __forceinline__ int window_below(int p, int window) {
     return (int)max((int64_t)p - window, (int64_t)-1);
 }
 
-__device__ __forceinline__ floatx16 mfma32x32x2(float a, float b, const floatx16& c) {
-    return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+__device__ __forceinline__ floatx4 mfma16x16x4(float a, float b, const floatx4& c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t chunk_rsrc(const void* base, uint32_t bytes) {
@@ -123,7 +127,10 @@ void k_attention_window(WinArgs a) {
     constexpr int kEs = (int)sizeof(T);
     __shared__ __attribute__((aligned(16))) uint8_t kvs[2 * kStage];
     const int wave = uni(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-    const int l32 = lane % 32, h2 = lane / 32;
+    // A lane holds scores of one row in each of RB blocks of LR rows, of the keys that its `part` says:
+    // score r is key 8 (r / 4) + 4 part + r % 4 in bf16 and 16 (r / 4) + 4 (r % 4) + part in fp32.
+    constexpr int RB = BF16 ? 1 : 2, LR = kWinBlock / RB, NS = 16 / RB;
+    const int lrow = lane % LR, part = lane / LR;
     // (a zero scale would turn hidden keys' -inf into NaN; below 1e-30 every exponential is 1 anyway)
     const float zs = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-30f);
     const bool flip = a.scale < 0.f;
@@ -144,9 +151,9 @@ void k_attention_window(WinArgs a) {
     const int32_t* const entry = a.av_items + 3 * min(it, a.av_cap - 1);
     const int errors = a.status[0], n_items = a.status[2], eb = entry[0], eh = entry[1], eti = entry[2];
     if (uni(errors) != 0 || it >= uni(n_items)) return;
-    const int b = uni(eb), h = uni(eh), ti = uni(eti);
-    const int len = a.lengths[b], off = a.tok_off[b], kvn = a.kv_len ? a.kv_len[b] : len;
-    const int64_t kv0 = a.kv_len ? a.kv_first[b] : off;
+    const int seq = uni(eb), h = uni(eh), ti = uni(eti);
+    const int len = a.lengths[seq], off = a.tok_off[seq], kvn = a.kv_len ? a.kv_len[seq] : len;
+    const int64_t kv0 = a.kv_len ? a.kv_first[seq] : off;
     const int L = uni(len), t0 = uni(off);
     const auto per_group = [&](int x) { return G == 1 ? x : (int)__umulhi((uint32_t)x, a.magic); };  // x / G, x < 2^16
     const int hk = uni(per_group(h)), rows = L * G;
@@ -179,14 +186,26 @@ void k_attention_window(WinArgs a) {
     // A row at position p sees the `range` keys from `from` on and those below sink_range.  Of the wave's rows: the
     // last chunk that any sees (-1: none) and the first of the windows; chunks [whole0, whole1)
     // are seen whole by all.
-    const int w0 = wave * kWinBlock, row = min(w0 + l32, rows - 1 - r0);
+    const int w0 = wave * kWinBlock;
     const bool active = r0 + w0 < rows;
-    const int tok = token(row), head = hk * G + (rem + row - (tok - tok0) * G);
-    const int p = past + tok, from = window_below(p, a.window) + 1;
-    const uint32_t range = (uint32_t)max(p + 1 - from, 0);
-    const int sink_range = min(a.sinks, p + 1);
+    int tok[RB], head[RB], p[RB], from[RB], sink_range[RB];
+    uint32_t range[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+        const int row = min(w0 + LR * b + lrow, rows - 1 - r0);
+        tok[b] = token(row);
+        head[b] = hk * G + (rem + row - (tok[b] - tok0) * G);
+        p[b] = past + tok[b];
+        from[b] = window_below(p[b], a.window) + 1;
+        range[b] = (uint32_t)max(p[b] + 1 - from[b], 0);
+        sink_range[b] = min(a.sinks, p[b] + 1);
+    }
     const int plo = past + uni(token(w0)), phi = past + uni(token(w0 + kWinBlock - 1));
     const int last = active && phi >= 0 ? phi / kWinChunk : -1, wfrom = window_below(plo, a.window) + 1, wfirst = wfrom / kWinChunk;
+    // of a block of LR rows: does any see one of the n keys from k0 on?
+    const int bhi[2] = {past + uni(token(w0 + LR - 1)), r0 + w0 + kWinBlock - LR < rows ? phi : -1};  // (-1: no rows)
+    const int bfrom[2] = {wfrom, window_below(past + uni(token(w0 + kWinBlock - LR)), a.window) + 1};
+    const auto block_sees = [&](int b, int k0, int n) { return k0 <= bhi[b] && (k0 + n > bfrom[b] || k0 < a.sinks); };
     const int whole0 = (window_below(phi, a.window) + kWinChunk) / kWinChunk, whole1 = plo >= 0 ? (plo + 1) / kWinChunk : 0;
 
     // copy i of this wave fills rows 1 KB apart from block wave * kBlocks + i of K and V;
@@ -215,84 +234,124 @@ void k_attention_window(WinArgs a) {
             copy_1k(rv, st + kWinChunk * W::kRow + blk * 1024, vvo[i2]);
         }
     };
-    // Q operand: bf16 k = 16 ks + 8 h2 .. of row l32; fp32 k = 8 u + 4 h2 + e
-    constexpr int kQ = BF16 ? 4 : 8;
-    u32x4 qf[kQ];
-    const T* const qrow = static_cast<const T*>(a.q) + (int64_t)(t0 + tok) * a.ldq + head * kHeadDim;
+    // Q operand: channels 16 u + 8 part .. in bf16, 16 u + 4 part + e in fp32
+    u32x4 qf[RB][4];
 #pragma unroll
-    for (int u = 0; u < kQ; ++u) {
-        qf[u] = active ? *reinterpret_cast<const u32x4*>(qrow + (BF16 ? 16 * u + 8 * h2 : 8 * u + 4 * h2)) : u32x4{0u, 0u, 0u, 0u};
-        if (flip) qf[u] ^= BF16 ? 0x80008000u : 0x80000000u;
+    for (int b = 0; b < RB; ++b) {
+        const T* const qrow = static_cast<const T*>(a.q) + (int64_t)(t0 + tok[b]) * a.ldq + head[b] * kHeadDim;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            qf[b][u] = active ? *reinterpret_cast<const u32x4*>(qrow + 16 * u + (BF16 ? 8 : 4) * part) : u32x4{0u, 0u, 0u, 0u};
+            if (flip) qf[b][u] ^= BF16 ? 0x80008000u : 0x80000000u;
+        }
     }
-    float m = -FLT_MAX, lsum = 0.f;
+    float m[RB], lsum[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) m[b] = -FLT_MAX, lsum[b] = 0.f;
     int fresh = 1;  // no chunk yet (a bool would be a lane mask)
     bool infinite = false;  // a chunk with hidden keys held values that are not finite
-    floatx16 oacc[2];
+    // O^T: NO blocks of WO channels (32 of one row block, 16 of each of two); register e of block cb is channel
+    // WO cb + 8 (e / 4) + 4 part + e % 4
+    constexpr int NO = BF16 ? 2 : 4, WO = kHeadDim / NO, EO = BF16 ? 16 : 4;
+    using Out = std::conditional_t<BF16, floatx16, floatx4>;
+    Out oacc[RB][NO];
 #pragma unroll
-    for (int cb = 0; cb < 2; ++cb)
+    for (int b = 0; b < RB; ++b)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) oacc[cb][r] = 0.f;
+        for (int cb = 0; cb < NO; ++cb)
+#pragma unroll
+            for (int e = 0; e < EO; ++e) oacc[b][cb][e] = 0.f;
 
-    const auto sees = [&](int j) { return ((uint32_t)(j - from) < range) | (j < sink_range); };
+    const auto sees = [&](int b, int j) { return ((uint32_t)(j - from[b]) < range[b]) | (j < sink_range[b]); };
     // One chunk of the stage at byte `stage`; `whole`: every row sees all of it.
     const auto work = [&](int c, bool whole, auto stg) {
         constexpr int stage = decltype(stg)::value;
         const int c0 = c * kWinChunk;
         const uint8_t* const kst = kvs + stage;
         const uint8_t* const vst = kst + kWinChunk * W::kRow;
-        floatx16 acc;
+        float sc[RB][NS];
         // (`again`: the rare recomputation, where V is already held and K is read as registers allow)
         const auto products = [&](auto again) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[r] = 0.f;
             if constexpr (BF16) {
                 const uint16_t* const ks = reinterpret_cast<const uint16_t*>(kst);
                 u32x4 kf[4];
+                floatx16 acc;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) kf[u] = *reinterpret_cast<const u32x4*>(ks + kv_off(l32, 16 * u + 8 * h2));
+                for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) kf[u] = *reinterpret_cast<const u32x4*>(ks + kv_off(lrow, 16 * u + 8 * part));
                 if constexpr (!decltype(again)::value) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int u = 0; u < 4; ++u) acc = mfma32x32x16(as_bf16x8(kf[u]), as_bf16x8(qf[u]), acc);
+                for (int u = 0; u < 4; ++u) acc = mfma32x32x16(as_bf16x8(kf[u]), as_bf16x8(qf[0][u]), acc);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sc[0][r] = acc[r];
             } else {
+                // 16 keys by 16 rows at a time, where any row sees a key of them; operand row i is key 4 (i % 4) + i / 4
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const floatx4 kf = *reinterpret_cast<const floatx4*>(kst + l32 * W::kRow + (((2 * u + h2) ^ W::swz(l32)) * 16));
-                    const floatx4 q4 = __builtin_bit_cast(floatx4, qf[u]);
+                for (int kb = 0; kb < 2; ++kb) {
+                    const int kk = 16 * kb + 4 * (lrow % 4) + lrow / 4;
+                    floatx4 kf[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc = mfma32x32x2(kf[e], q4[e], acc);
+                    for (int u = 0; u < 4; ++u)
+                        kf[u] = *reinterpret_cast<const floatx4*>(kst + kk * W::kRow + (((4 * u + part) ^ W::swz(kk)) * 16));
+                    floatx4 acc[RB];
+                    const auto multiply = [&](int b0, int b1) {
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                                for (int b = b0; b < b1; ++b) acc[b] = mfma16x16x4(kf[u][e], __builtin_bit_cast(floatx4, qf[b][u])[e], acc[b]);
+                    };
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) acc[b] = floatx4{0.f, 0.f, 0.f, 0.f};
+                    const bool first = block_sees(0, c0 + 16 * kb, 16), second = block_sees(1, c0 + 16 * kb, 16);
+                    if (first && second) multiply(0, 2);  // (two chains of dependent products in turn)
+                    else if (first) multiply(0, 1);
+                    else if (second) multiply(1, 2);
+#pragma unroll
+                    for (int b = 0; b < RB; ++b)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) sc[b][4 * kb + r] = acc[b][r];
                 }
             }
         };
         const auto hide = [&] {
             if (!whole) {
-                // bit j: key c0 + 4 h2 + j is seen
+                // bit j: key c0 + j (past the part's first) is seen
                 const auto below = [](int n) { return n >= 32 ? ~0u : ~(~0u << max(n, 0)); };
-                const uint32_t seen = ((below(p + 1 - c0) & ~below(from - c0)) | below(sink_range - c0)) >> (4 * h2);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const uint32_t all = (uint32_t)__builtin_amdgcn_sbfe((int)seen, 8 * (r / 4) + r % 4, 1);  // or no bits
-                    acc[r] = __uint_as_float((all & __float_as_uint(acc[r])) | (~all & 0xff800000u));
+                for (int b = 0; b < RB; ++b) {
+                    const uint32_t seen = ((below(p[b] + 1 - c0) & ~below(from[b] - c0)) | below(sink_range[b] - c0)) >> (BF16 ? 4 * part : part);
+#pragma unroll
+                    for (int r = 0; r < NS; ++r) {
+                        const uint32_t all = (uint32_t)__builtin_amdgcn_sbfe((int)seen, BF16 ? 8 * (r / 4) + r % 4 : 16 * (r / 4) + 4 * (r % 4), 1);  // or no bits
+                        sc[b][r] = __uint_as_float((all & __float_as_uint(sc[b][r])) | (~all & 0xff800000u));
+                    }
                 }
             }
         };
-        const auto chunk_max = [&] {
-            float cmax = acc[0];
+        const auto chunk_max = [&](int b) {
+            float cmax = sc[b][0];
 #pragma unroll
-            for (int r = 1; r < 16; ++r) cmax = fmaxf(cmax, acc[r]);
+            for (int r = 1; r < NS; ++r) cmax = fmaxf(cmax, sc[b][r]);
+            if constexpr (!BF16) cmax = fmaxf(cmax, __shfl_xor(cmax, 16));
             return max_xor32(cmax) * zs;
         };
-        const auto exps = [&] {
+        const auto exps = [&](int b) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[r] = __builtin_amdgcn_exp2f(fmaf(acc[r], zs, -m));
-            float s[8];
+            for (int r = 0; r < NS; ++r) sc[b][r] = __builtin_amdgcn_exp2f(fmaf(sc[b][r], zs, -m[b]));
+            float t[NS / 2];
 #pragma unroll
-            for (int r = 0; r < 8; ++r) s[r] = acc[2 * r] + acc[2 * r + 1];
+            for (int r = 0; r < NS / 2; ++r) t[r] = sc[b][2 * r] + sc[b][2 * r + 1];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) s[r] += s[r + 4];
-            return (s[0] + s[2]) + (s[1] + s[3]);
+            for (int d = NS / 4; d > 0; d /= 2)
+#pragma unroll
+                for (int r = 0; r < d; ++r) t[r] += t[r + d];
+            return t[0];
         };
         products(std::false_type{});
-        // V^T operand: the lane's keys 16 t + {4 h2 .. + 3, 8 + 4 h2 .. + 3} of channel 32 cb + l32, by transposed
+        // V^T operand: the lane's keys 16 t + {4 part .. + 3, 8 + 4 part .. + 3} of channel 32 cb + lrow, by transposed
         // reads whose latency passes under the products above (inline assembly, its own wait
         // included: at the builtin the compiler waits for every copy into LDS, the next chunk's
         // too)
@@ -317,25 +376,38 @@ void k_attention_window(WinArgs a) {
         }
         hide();
         fresh = uni(fresh);
-        if (fresh) m = fmaxf(chunk_max(), -FLT_MAX);  // (no visible key: any later score is far above)
-        float ps = exps();
+        if (fresh) {  // (no visible key: any later score is far above)
+#pragma unroll
+            for (int b = 0; b < RB; ++b) m[b] = fmaxf(chunk_max(b), -FLT_MAX);
+        }
+        float ps[RB];
+        bool over = false;
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+            ps[b] = exps(b);
+            over |= !(ps[b] <= kSumCap);
+        }
         // a lane sum above kSumCap (or NaN) means a score well above m: raise m to the
         // chunk's maximum and rescale what has been summed
-        if (!fresh && __ballot(!(ps <= kSumCap)) != 0) {
+        if (!fresh && __ballot(over) != 0) {
             products(std::true_type{});
             hide();
-            const float mn = fmaxf(m, chunk_max());
-            const float alpha = __builtin_amdgcn_exp2f(m - mn);
-            lsum *= alpha;
 #pragma unroll
-            for (int cb = 0; cb < 2; ++cb)
+            for (int b = 0; b < RB; ++b) {
+                const float mn = fmaxf(m[b], chunk_max(b));
+                const float alpha = __builtin_amdgcn_exp2f(m[b] - mn);
+                lsum[b] *= alpha;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) oacc[cb][r] *= alpha;
-            m = mn;
-            ps = exps();
+                for (int cb = 0; cb < NO; ++cb)
+#pragma unroll
+                    for (int e = 0; e < EO; ++e) oacc[b][cb][e] *= alpha;
+                m[b] = mn;
+                ps[b] = exps(b);
+            }
         }
         fresh = 0;
-        lsum += ps;
+#pragma unroll
+        for (int b = 0; b < RB; ++b) lsum[b] += ps[b];
         // Values that are not finite, among hidden keys, would reach every row (0 times infinity): they
         // are taken out of the operand here and added after the last chunk.
         if constexpr (BF16) {
@@ -361,44 +433,47 @@ void k_attention_window(WinArgs a) {
             for (int t = 0; t < 2; ++t) {
                 u32x4 pw;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) pw[e] = pack_bf16x2(acc[8 * t + 2 * e], acc[8 * t + 2 * e + 1]);
+                for (int e = 0; e < 4; ++e) pw[e] = pack_bf16x2(sc[0][8 * t + 2 * e], sc[0][8 * t + 2 * e + 1]);
 #pragma unroll
                 for (int cb = 0; cb < 2; ++cb)
-                    oacc[cb] = mfma32x32x16(as_bf16x8(u32x4{tr[t][cb][0][0], tr[t][cb][0][1], tr[t][cb][1][0], tr[t][cb][1][1]}),
-                                            as_bf16x8(pw), oacc[cb]);
+                    oacc[0][cb] = mfma32x32x16(as_bf16x8(u32x4{tr[t][cb][0][0], tr[t][cb][0][1], tr[t][cb][1][0], tr[t][cb][1][1]}),
+                                               as_bf16x8(pw), oacc[0][cb]);
             }
             __builtin_amdgcn_s_setprio(0);
         } else {
-            // the lane's keys 8 (r / 4) + 4 h2 + r % 4 of channel 32 cb + l32
-            float vf[2][16];
-            bool bad = false;
+            // keys 4 r + part of channel 16 cb + lrow
+            float vf[NS][NO];
 #pragma unroll
-            for (int cb = 0; cb < 2; ++cb)
+            for (int r = 0; r < NS; ++r)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int kk = 8 * (r / 4) + 4 * h2 + (r % 4), ch = 32 * cb + l32;
-                    vf[cb][r] = *reinterpret_cast<const float*>(vst + kk * W::kRow + (((ch >> 2) ^ W::swz(kk)) * 16) + (ch & 3) * 4);
-                    bad |= !finite_f32(vf[cb][r]);
+                for (int cb = 0; cb < NO; ++cb) {
+                    const int kk = 4 * r + part, ch = 16 * cb + lrow;
+                    vf[r][cb] = *reinterpret_cast<const float*>(vst + kk * W::kRow + (((ch >> 2) ^ W::swz(kk)) * 16) + (ch & 3) * 4);
                 }
-            if (!whole && __ballot(bad) != 0) {
-                infinite = true;
+            if (!whole) {
+                uint32_t top = 0;  // largest magnitude's bits (those of values that are not finite from 0x7f800000 on)
 #pragma unroll
-                for (int cb = 0; cb < 2; ++cb)
+                for (int r = 0; r < NS; ++r)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (!finite_f32(vf[cb][r])) vf[cb][r] = 0.f;
+                    for (int cb = 0; cb < NO; ++cb) top = max(top, __float_as_uint(vf[r][cb]) & 0x7fffffffu);
+                if (__ballot(top >= 0x7f800000u) != 0) {
+                    infinite = true;
+#pragma unroll
+                    for (int r = 0; r < NS; ++r)
+#pragma unroll
+                        for (int cb = 0; cb < NO; ++cb)
+                            if (!finite_f32(vf[r][cb])) vf[r][cb] = 0.f;
+                }
             }
-            // groups of eight keys; those that no row of the wave sees are left out (a chunk of four sinks
-            // is two thirds of one)
+            // four keys at a time, where any row of the block sees one
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int k0 = c0 + 8 * g;
-                if (k0 > phi || (k0 + 7 < wfrom && k0 >= a.sinks)) continue;
+            for (int r = 0; r < NS; ++r)
 #pragma unroll
-                for (int r = 4 * g; r < 4 * g + 4; ++r)
+                for (int b = 0; b < RB; ++b) {
+                    if (!block_sees(b, c0 + 4 * r, 4)) continue;
 #pragma unroll
-                    for (int cb = 0; cb < 2; ++cb) oacc[cb] = mfma32x32x2(vf[cb][r], acc[r], oacc[cb]);
-            }
+                    for (int cb = 0; cb < NO; ++cb) oacc[b][cb] = mfma16x16x4(vf[r][cb], sc[b][r], oacc[b][cb]);
+                }
         }
     };
     const auto step = [&](int i, auto stg) {
@@ -420,48 +495,58 @@ void k_attention_window(WinArgs a) {
             const int c = chunk(i);
             if (c >= whole0 && c < whole1) continue;  // its products took them as they are
             for (int j = c * kWinChunk; j < (c + 1) * kWinChunk; ++j) {
-                if (!sees(j)) continue;
-                const T* const vrow = vbase + (int64_t)j * a.ldv + 4 * h2;
+                const T* const vrow = vbase + (int64_t)j * a.ldv + 4 * part;
 #pragma unroll
-                for (int cb = 0; cb < 2; ++cb)
+                for (int b = 0; b < RB; ++b) {
+                    if (!sees(b, j)) continue;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        float x;
-                        if constexpr (BF16) x = bf16_to_f32(vrow[32 * cb + 8 * (r / 4) + r % 4]);
-                        else x = vrow[32 * cb + 8 * (r / 4) + r % 4];
-                        if (!finite_f32(x)) oacc[cb][r] += x;
-                    }
+                    for (int cb = 0; cb < NO; ++cb)
+#pragma unroll
+                        for (int e = 0; e < EO; ++e) {
+                            float x;
+                            if constexpr (BF16) x = bf16_to_f32(vrow[WO * cb + 8 * (e / 4) + e % 4]);
+                            else x = vrow[WO * cb + e];
+                            if (!finite_f32(x)) oacc[b][cb][e] += x;
+                        }
+                }
             }
         }
     }
-    float sum = sum_xor32(lsum);
-    if (r0 + w0 + l32 >= rows) return;
-    if (p < 0 || (a.window == 0 && a.sinks == 0)) sum = 1.f;  // the row sees nothing: its output is zero
-    const int64_t gr = (int64_t)(t0 + tok);
-    if (a.splits > 1) {
-        const int64_t slot = ((int64_t)blockIdx.y * a.T + gr) * a.heads + head;
-        float* const po = a.part_o + slot * kHeadDim;
 #pragma unroll
-        for (int cb = 0; cb < 2; ++cb)
+    for (int b = 0; b < RB; ++b) {
+        if constexpr (!BF16) lsum[b] += __shfl_xor(lsum[b], 16);
+        lsum[b] = sum_xor32(lsum[b]);
+    }
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<floatx4*>(po + 32 * cb + 8 * g + 4 * h2) =
-                    floatx4{oacc[cb][4 * g], oacc[cb][4 * g + 1], oacc[cb][4 * g + 2], oacc[cb][4 * g + 3]};
-        if (h2 == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * slot) = float2{m, sum};
-    } else {
-        const float inv = 1.0f / sum;
-        T* const orow = static_cast<T*>(a.out) + gr * a.ldo + head * kHeadDim;
+    for (int b = 0; b < RB; ++b) {
+        float sum = lsum[b];
+        if (r0 + w0 + LR * b + lrow >= rows) continue;
+        if (p[b] < 0 || (a.window == 0 && a.sinks == 0)) sum = 1.f;  // the row sees nothing: its output is zero
+        const int64_t gr = (int64_t)(t0 + tok[b]);
+        if (a.splits > 1) {
+            const int64_t slot = ((int64_t)blockIdx.y * a.T + gr) * a.heads + head[b];
+            float* const po = a.part_o + slot * kHeadDim;
 #pragma unroll
-        for (int cb = 0; cb < 2; ++cb)
+            for (int cb = 0; cb < NO; ++cb)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const float o0 = oacc[cb][4 * g] * inv, o1 = oacc[cb][4 * g + 1] * inv, o2 = oacc[cb][4 * g + 2] * inv,
-                            o3 = oacc[cb][4 * g + 3] * inv;
-                if constexpr (BF16)
-                    *reinterpret_cast<u32x2*>(orow + 32 * cb + 8 * g + 4 * h2) = u32x2{pack_bf16x2(o0, o1), pack_bf16x2(o2, o3)};
-                else
-                    *reinterpret_cast<floatx4*>(orow + 32 * cb + 8 * g + 4 * h2) = floatx4{o0, o1, o2, o3};
-            }
+                for (int g = 0; g < EO / 4; ++g)
+                    *reinterpret_cast<floatx4*>(po + WO * cb + 8 * g + 4 * part) =
+                        floatx4{oacc[b][cb][4 * g], oacc[b][cb][4 * g + 1], oacc[b][cb][4 * g + 2], oacc[b][cb][4 * g + 3]};
+            if (part == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * slot) = float2{m[b], sum};
+        } else {
+            const float inv = 1.0f / sum;
+            T* const orow = static_cast<T*>(a.out) + gr * a.ldo + head[b] * kHeadDim;
+#pragma unroll
+            for (int cb = 0; cb < NO; ++cb)
+#pragma unroll
+                for (int g = 0; g < EO / 4; ++g) {
+                    const float o0 = oacc[b][cb][4 * g] * inv, o1 = oacc[b][cb][4 * g + 1] * inv, o2 = oacc[b][cb][4 * g + 2] * inv,
+                                o3 = oacc[b][cb][4 * g + 3] * inv;
+                    T* const dst = orow + WO * cb + 8 * g + 4 * part;
+                    if constexpr (BF16) *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(o0, o1), pack_bf16x2(o2, o3)};
+                    else *reinterpret_cast<floatx4*>(dst) = floatx4{o0, o1, o2, o3};
+                }
+        }
     }
 }
 
