@@ -42,8 +42,8 @@ RAG_ROTARY_MAX_DIM = 512
 VGEMM_DATA_BITS = {1: "negative size", 2: "size > RAG_VGEMM_MAX_DIM", 4: "tile_cap exceeded",
                    8: "operand buffer too small", 16: "bf16 needs k % 64 == 0 and n % 8 == 0"}
 
-if not os.path.exists(LIB_PATH):
-    raise ImportError(f"{LIB_PATH} is missing: build the HIP library first "
+if not os.path.exists(LIB_PATH) or not os.path.exists(os.path.join(_HERE, "_binding.so")):
+    raise ImportError(f"{LIB_PATH} or _binding.so is missing: build the HIP library first "
                       "(python paper_2110_10221_amd/_build.py)")
 
 _lib = ctypes.CDLL(LIB_PATH)
@@ -276,9 +276,15 @@ def packed_layernorm(x, gamma, beta, y, eps=1e-5, stream=None):
                                             _dtype_code(x), _stream(stream)))
 
 
-# The operators below check types, shapes and devices of what they are given; a step of
-# single tokens takes as long as its host side, so the checks are one comparison each and
-# pointers go to ctypes as integers.
+# The operators below check types, shapes and devices of what they are given.  A step of single tokens
+# takes as long as its host side, so calls whose arguments are as documented are read, checked and
+# made by _binding.so (packed_rmsnorm of 8 x 1024, call after call: 3.5 us, 6.4 by way of ctypes); it returns None, and
+# launches nothing, for any other call, which then meets the checks written out here.
+
+from . import _binding as _fast  # noqa: E402
+
+_fast.bind(torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
+           *(ctypes.cast(f, _p).value for f in (_c_rmsnorm, _c_quantize_i8, _c_linear_i8, _c_rotary, _c_window, _c_window_cached)))
 
 class _Codes(dict):
     def __missing__(self, dtype):
@@ -327,25 +333,40 @@ def _launch_stream(stream, dev, plan=None):
 _I32_MAX = 2 ** 31 - 1  # (ctypes would wrap a larger window; no position passes it)
 
 
+def _sizes(*n):
+    """The sizes themselves: ctypes would wrap larger ones."""
+    if max(n) > _I32_MAX:
+        raise ValueError(f"sizes {n} pass 2^31 - 1")
+    return n
+
+
 def packed_rmsnorm(x, gamma, y=None, eps=1e-6, residual=None, x_out=None, q=None, q_scale=None, stream=None):
     """h = x + residual, and its RMS norm times gamma: into `y`, into the 8-bit rows `q` (int8)
     and `q_scale` (float32 [T]), or both; `x_out` receives h.  `y` and `x_out` may be x or residual."""
-    shape, dt, dev = x.shape, x.dtype, x.get_device()
-    T, d = shape
-    st = _c_rmsnorm(x.data_ptr(), _mat("x", x, shape, dt, dev), _addr(residual), _mat("residual", residual, shape, dt, dev),
-                    _vec("gamma", gamma, d, dt, dev), eps, _addr(x_out), _mat("x_out", x_out, shape, dt, dev),
-                    _addr(y), _mat("y", y, shape, dt, dev), _addr(q), _mat("q", q, shape, torch.int8, dev),
-                    _vec("q_scale", q_scale, T, torch.float32, dev), T, d, _CODES[dt], _launch_stream(stream, dev))
+    st = _fast.packed_rmsnorm(x, gamma, y, eps, residual, x_out, q, q_scale, stream)
+    if st is None:
+        st = _checked_rmsnorm(x, gamma, y, eps, residual, x_out, q, q_scale, stream)
     if st:
         _check("packed_rmsnorm", st)
 
 
+def _checked_rmsnorm(x, gamma, y, eps, residual, x_out, q, q_scale, stream):
+    shape, dt, dev = x.shape, x.dtype, x.get_device()
+    T, d = _sizes(*shape)
+    return _c_rmsnorm(x.data_ptr(), _mat("x", x, shape, dt, dev), _addr(residual), _mat("residual", residual, shape, dt, dev),
+                      _vec("gamma", gamma, d, dt, dev), eps, _addr(x_out), _mat("x_out", x_out, shape, dt, dev),
+                      _addr(y), _mat("y", y, shape, dt, dev), _addr(q), _mat("q", q, shape, torch.int8, dev),
+                      _vec("q_scale", q_scale, T, torch.float32, dev), T, d, _CODES[dt], _launch_stream(stream, dev))
+
+
 def packed_quantize_i8(x, q, scale, stream=None):
     """8-bit rows of x [T, d] (tokens, or a weight matrix): q int8 [T, d], scale float32 [T]."""
-    shape, dt, dev = x.shape, x.dtype, x.get_device()
-    T, d = shape
-    st = _c_quantize_i8(x.data_ptr(), _mat("x", x, shape, dt, dev), _addr(q), _mat("q", q, shape, torch.int8, dev),
-                        _vec("scale", scale, T, torch.float32, dev), T, d, _CODES[dt], _launch_stream(stream, dev))
+    st = _fast.packed_quantize_i8(x, q, scale, stream)
+    if st is None:
+        shape, dt, dev = x.shape, x.dtype, x.get_device()
+        T, d = _sizes(*shape)
+        st = _c_quantize_i8(x.data_ptr(), _mat("x", x, shape, dt, dev), _addr(q), _mat("q", q, shape, torch.int8, dev),
+                            _vec("scale", scale, T, torch.float32, dev), T, d, _CODES[dt], _launch_stream(stream, dev))
     if st:
         _check("packed_quantize_i8", st)
 
@@ -353,17 +374,22 @@ def packed_quantize_i8(x, q, scale, stream=None):
 def packed_linear_i8(x, x_scale, w, w_scale, y, bias=None, residual=None, act=RAG_ACT_NONE, stream=None):
     """y = act(x_scale w_scale (x w^T) + bias) + residual: x int8 [T, K] and w int8 [N, K] in 8-bit rows with
     their float32 scales ([T] and [N]); bias, residual and y (which may be residual) of one type."""
-    dt, dev = y.dtype, y.get_device()
-    T, K = x.shape
-    N = w.shape[0]
-    if _mat("w", w, (N, K), torch.int8, dev) != K and N > 1:
-        raise ValueError("w must be contiguous")
-    st = _c_linear_i8(x.data_ptr(), _mat("x", x, (T, K), torch.int8, dev), _vec("x_scale", x_scale, T, torch.float32, dev),
-                      w.data_ptr(), _vec("w_scale", w_scale, N, torch.float32, dev), _vec("bias", bias, N, dt, dev),
-                      _addr(residual), _mat("residual", residual, (T, N), dt, dev), act, y.data_ptr(),
-                      _mat("y", y, (T, N), dt, dev), T, K, N, _CODES[dt], _launch_stream(stream, dev))
+    st = _fast.packed_linear_i8(x, x_scale, w, w_scale, y, bias, residual, act, stream)
+    if st is None:
+        st = _checked_linear_i8(x, x_scale, w, w_scale, y, bias, residual, act, stream)
     if st:
         _check("packed_linear_i8", st)
+
+
+def _checked_linear_i8(x, x_scale, w, w_scale, y, bias, residual, act, stream):
+    dt, dev = y.dtype, y.get_device()
+    T, K, N = _sizes(*x.shape, w.shape[0])
+    if _mat("w", w, (N, K), torch.int8, dev) != K and N > 1:
+        raise ValueError("w must be contiguous")
+    return _c_linear_i8(x.data_ptr(), _mat("x", x, (T, K), torch.int8, dev), _vec("x_scale", x_scale, T, torch.float32, dev),
+                        w.data_ptr(), _vec("w_scale", w_scale, N, torch.float32, dev), _vec("bias", bias, N, dt, dev),
+                        _addr(residual), _mat("residual", residual, (T, N), dt, dev), act, y.data_ptr(),
+                        _mat("y", y, (T, N), dt, dev), T, K, N, _CODES[dt], _launch_stream(stream, dev))
 
 
 def rotary_frequencies(rot_dim, base=10000.0, scaling=RAG_ROTARY_PLAIN, factor=1.0, orig_len=0, beta_fast=32.0,
@@ -381,12 +407,15 @@ def packed_rotary(plan: Plan, x, y, inv_freq, heads, head_dim=RAG_HEAD_DIM, layo
     """Turns the first 2 * len(inv_freq) channels of each of `heads` heads of x [T, heads * head_dim] into y (which
     may be x).  inv_freq is a float64 device tensor; pos_start int32 [B] holds each sequence's first position;
     `inverse` turns back."""
-    dt, dev, n = x.dtype, x.get_device(), inv_freq.numel()
-    shape = (plan.total_tokens, heads * head_dim)
-    st = _c_rotary(plan.ref(), x.data_ptr(), _mat("x", x, shape, dt, dev), y.data_ptr(), _mat("y", y, shape, dt, dev), heads,
-                   head_dim, 2 * n, layout | (RAG_ROTARY_INVERSE if inverse else 0),
-                   _vec("inv_freq", inv_freq, n, torch.float64, dev), amplitude,
-                   _vec("pos_start", pos_start, plan.batch, torch.int32, dev), _CODES[dt], _launch_stream(stream, dev, plan))
+    st = _fast.packed_rotary(plan, x, y, inv_freq, heads, head_dim, layout, amplitude, pos_start, inverse, stream)
+    if st is None:
+        dt, dev, n = x.dtype, x.get_device(), inv_freq.numel()
+        shape = (plan.total_tokens, heads * head_dim)
+        _sizes(2 * n)
+        st = _c_rotary(plan.ref(), x.data_ptr(), _mat("x", x, shape, dt, dev), y.data_ptr(), _mat("y", y, shape, dt, dev), heads,
+                       head_dim, 2 * n, layout | (RAG_ROTARY_INVERSE if inverse else 0),
+                       _vec("inv_freq", inv_freq, n, torch.float64, dev), amplitude,
+                       _vec("pos_start", pos_start, plan.batch, torch.int32, dev), _CODES[dt], _launch_stream(stream, dev, plan))
     if st:
         _check("packed_rotary", st)
 
@@ -416,10 +445,13 @@ def ragged_attention_window(plan: Plan, q, k, v, out, scale, window, sinks=0, kv
                             workspace=None, stream=None):
     """Causal attention over the packed batch: position p sees keys j <= p with j > p - window or j < sinks.
     k and v hold kv_heads (default: all) heads, each shared by plan.heads / kv_heads query heads."""
-    kvh = kv_heads or plan.heads
-    code, dev, ld, ws, n = _window_operands(plan, q, k, v, out, plan.total_tokens, kvh, head_dim, workspace)
-    st = _c_window(plan.ref(), q.data_ptr(), ld[0], k.data_ptr(), ld[1], v.data_ptr(), ld[2], kvh, head_dim, scale,
-                   min(window, _I32_MAX), min(sinks, _I32_MAX), out.data_ptr(), ld[3], ws, n, code, _launch_stream(stream, dev, plan))
+    st = _fast.ragged_attention_window(plan, q, k, v, out, scale, window, sinks, kv_heads, head_dim, workspace, stream)
+    if st is None:
+        kvh = kv_heads or plan.heads
+        code, dev, ld, ws, n = _window_operands(plan, q, k, v, out, plan.total_tokens, kvh, head_dim, workspace)
+        st = _c_window(plan.ref(), q.data_ptr(), ld[0], k.data_ptr(), ld[1], v.data_ptr(), ld[2], kvh, head_dim, scale,
+                       min(window, _I32_MAX), min(sinks, _I32_MAX), out.data_ptr(), ld[3], ws, n, code,
+                       _launch_stream(stream, dev, plan))
     if st:
         _check("ragged_attention_window", st)
 
@@ -428,12 +460,16 @@ def ragged_attention_window_cached(plan: Plan, q, k, v, kv_first, kv_len, max_kv
                                    kv_heads=None, head_dim=RAG_HEAD_DIM, workspace=None, stream=None):
     """The same over caches k and v [rows, kv_heads * head_dim]: sequence b's keys are the kv_len[b] rows from
     kv_first[b] (int32 and int64 device tensors), its queries the last plan.lengths[b] of those positions."""
-    kvh, rows = kv_heads or plan.heads, k.shape[0]
-    code, dev, ld, ws, n = _window_operands(plan, q, k, v, out, rows, kvh, head_dim, workspace)
-    st = _c_window_cached(plan.ref(), q.data_ptr(), ld[0], k.data_ptr(), ld[1], v.data_ptr(), ld[2], rows,
-                          _vec("kv_first", kv_first, plan.batch, torch.int64, dev),
-                          _vec("kv_len", kv_len, plan.batch, torch.int32, dev), min(max_kv_len, _I32_MAX), kvh,
-                          head_dim, scale, min(window, _I32_MAX), min(sinks, _I32_MAX), out.data_ptr(), ld[3], ws, n, code, _launch_stream(stream, dev, plan))
+    st = _fast.ragged_attention_window_cached(plan, q, k, v, kv_first, kv_len, max_kv_len, out, scale, window, sinks, kv_heads,
+                                              head_dim, workspace, stream)
+    if st is None:
+        kvh, rows = kv_heads or plan.heads, k.shape[0]
+        code, dev, ld, ws, n = _window_operands(plan, q, k, v, out, rows, kvh, head_dim, workspace)
+        st = _c_window_cached(plan.ref(), q.data_ptr(), ld[0], k.data_ptr(), ld[1], v.data_ptr(), ld[2], rows,
+                              _vec("kv_first", kv_first, plan.batch, torch.int64, dev),
+                              _vec("kv_len", kv_len, plan.batch, torch.int32, dev), min(max_kv_len, _I32_MAX), kvh,
+                              head_dim, scale, min(window, _I32_MAX), min(sinks, _I32_MAX), out.data_ptr(), ld[3], ws, n, code,
+                              _launch_stream(stream, dev, plan))
     if st:
         _check("ragged_attention_window_cached", st)
 

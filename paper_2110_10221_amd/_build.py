@@ -1,7 +1,8 @@
 """Build libragged.so (the HIP kernels and the C interface) for gfx950 with hipcc.
 
 Each source compiles to its own object in parallel; the objects link into one
-shared library placed next to this file, where the binding loads it.
+shared library placed next to this file, where the binding loads it.  The binding's own
+compiled part (_binding.so, host code against torch's headers) is built beside it.
 """
 from __future__ import annotations
 
@@ -15,6 +16,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libragged.so")
+BINDING = os.path.join(HERE, "_binding.so")
 OBJ_DIR = os.path.join(ROOT, "_build", "ragged")
 
 SOURCES = ["api.cpp", "offsets.hip", "attention.hip", "attention_window.hip", "gemm.hip", "gemm_f32.hip", "gemm_small.hip", "gemm_big.hip", "gemm_i8.hip",
@@ -48,6 +50,25 @@ def _compile(src: str, defines=(), obj_dir: str = OBJ_DIR, sanitize: bool = Fals
     return obj
 
 
+def _build_binding() -> str:
+    import sysconfig
+
+    import torch
+
+    base = os.path.dirname(torch.__file__)
+    tmp = BINDING + ".tmp"
+    cmd = [shutil.which("g++") or hipcc(), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I", INCLUDE,
+           "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(base, "include"),
+           os.path.join(CSRC, "binding.cpp"), "-o", tmp,
+           "-L" + os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"building the binding failed:\n{' '.join(cmd)}\n{res.stdout}\n{res.stderr}")
+    os.replace(tmp, BINDING)
+    return BINDING
+
+
 def build(jobs: int | None = None, out: str = LIB, defines=(), sanitize: bool = False) -> str:
     """Compile and link; `out` and `defines` (extra -D flags) serve alternate builds;
     `sanitize` instruments the host code with AddressSanitizer and
@@ -59,7 +80,10 @@ def build(jobs: int | None = None, out: str = LIB, defines=(), sanitize: bool = 
     os.makedirs(obj_dir, exist_ok=True)
     jobs = jobs or min(len(SOURCES), os.cpu_count() or 4)
     with concurrent.futures.ThreadPoolExecutor(jobs) as ex:
-        objs = list(ex.map(lambda src: _compile(src, defines, obj_dir, sanitize), SOURCES))
+        objs = ex.map(lambda src: _compile(src, defines, obj_dir, sanitize), SOURCES)
+        if out == LIB and not sanitize:
+            _build_binding()
+        objs = list(objs)
     tmp = out + ".tmp"
     cmd = [hipcc(), "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp] + (SANITIZE if sanitize else []) + objs
     res = subprocess.run(cmd, capture_output=True, text=True)
