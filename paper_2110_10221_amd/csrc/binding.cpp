@@ -233,6 +233,7 @@ template <PyObject* (*f)(PyObject* const*), Py_ssize_t n>
 PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t got) {
     if (got != n) return PyErr_Format(PyExc_TypeError, "%zd arguments, not %zd", n, got);
     try {
+        need(current_device != nullptr);  // (bound)
         return f(args);
     } catch (...) {  // (NotPlain, or torch's own error)
         PyErr_Clear();

@@ -28,6 +28,21 @@ def test_arguments_of_any_kind_are_left_to_python(name, n):
         f(*[None] * (n - 1))
 
 
+def test_sizes_past_32_bits_are_refused():
+    import paper_2110_10221_amd as rag
+
+    n = 2 ** 32 + 5
+    x, q, v = torch.zeros(1, 64).expand(n, 64), torch.zeros(1, 64, dtype=torch.int8).expand(n, 64), torch.zeros(1).expand(n)
+    with pytest.raises(ValueError, match="2.31"):
+        rag.packed_rmsnorm(x, torch.zeros(64), x)
+    with pytest.raises(ValueError, match="2.31"):
+        rag.packed_quantize_i8(x, q, v)
+    with pytest.raises(ValueError, match="2.31"):
+        rag.packed_linear_i8(q, v, q[:8], v[:8], x)
+    with pytest.raises(ValueError, match="2.31"):
+        rag.packed_linear_i8(q[:8], v[:8], q, v, x[:8])
+
+
 def calls(T=6, d=64):
     """{name: (arguments, {position: values that are not as documented})}, on the GPU."""
     import paper_2110_10221_amd as rag
