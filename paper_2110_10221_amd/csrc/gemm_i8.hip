@@ -434,12 +434,29 @@ hipError_t launch_few(const I8Args& a, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Tiles of 32 tokens.  Where they are fewer than the CUs each CU runs one at its own copies' latency: 32
+// features if that many tiles still fit one round, and six stages (us with 64 features and four stages, as the other
+// calls run, and so: 32 x 4096 x 4096 11.1, 8.2; 64 x 8192 x 2048 18.3, 12.4; 32 x 1024 x 1024 3.9, 3.8;
+// with 64 features and six 100 x 4096 x 4096 10.7, 8.8; 160 x 1024 x 4096, more tiles than CUs, 5.0, 5.5).
+template <bool BF16, int ACT>
+hipError_t launch_tiles32(const I8Args& a, int cus, hipStream_t s) {
+    const int64_t rows = ((int64_t)a.T + 31) / 32;
+    if (rows * (((int64_t)a.N + 31) / 32) <= cus) return launch_tiles<I8Cfg<32, 32, 1, 1, 2, 6>, BF16, ACT>(a, s);
+    if (rows * (((int64_t)a.N + 63) / 64) <= cus) return launch_tiles<I8Cfg<32, 64, 1, 2, 2, 6>, BF16, ACT>(a, s);
+    return launch_tiles<I8Cfg<32, 64, 1, 2, 2, 4>, BF16, ACT>(a, s);
+}
+
 template <bool BF16, int ACT>
 hipError_t launch_form(const I8Args& a, hipStream_t s) {
     const int cus = device_cu_count();
     switch (linear_form_i8(a.T, a.K, a.N, ACT, BF16, cus)) {
-        case 0: return launch_few<BF16, ACT>(a, s);
-        case 1: return launch_tiles<I8Cfg<32, 64, 1, 2, 2, 4>, BF16, ACT>(a, s);
+        case 0:
+            // its workgroups read all of x for 16 features each: with more than a few tokens and a GPU full of tiles
+            // those are faster (us at 1, 8 and 16 tokens, and on tiles at any of them: 8192 x 8192 15.5, 16.8, 19.7, and
+            // 15.4; 4096 x 16384 15.3, 17.2, 20.9, and 16.8)
+            if (a.T > 4 && a.N >= 32 * cus) return launch_tiles32<BF16, ACT>(a, cus, s);
+            return launch_few<BF16, ACT>(a, s);
+        case 1: return launch_tiles32<BF16, ACT>(a, cus, s);
         case 2: return launch_tiles<I8Cfg<64, 64, 2, 2, 1, 3>, BF16, ACT>(a, s);
         case 3: return launch_tiles<I8Cfg<64, 128, 2, 2, 1, 3>, BF16, ACT>(a, s);
         case 4: return launch_tiles<I8Cfg<128, 128, 2, 4, 1, 2>, BF16, ACT>(a, s);
@@ -458,7 +475,7 @@ hipError_t launch_type(const I8Args& a, int act, hipStream_t s) {
 
 }  // namespace
 
-// The form of a call: 0 few tokens, 1 .. 4 the tiles 32 x 64 (two k shares), 64 x 64, 64 x 128
+// The form of a call: 0 few tokens, 1 .. 4 the tiles of 32 tokens (two k shares), 64 x 64, 64 x 128
 // and 128 x 128, 5 the 256 x 256 tiles and quarters.  Up to 16 tokens the first one (T = 16, K = N =
 // 4096: 6.7 us, 7.7 on 32 x 64 tiles; T = 32: 8.6 and 7.9).  Above, the smallest of the modelled times
 // in us

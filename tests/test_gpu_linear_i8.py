@@ -169,3 +169,13 @@ def test_every_form(T, K, N, form, form32):
     assert f(T, K, N, 0, True, 256) == form and f(T, K, N, 2, False, 256) == form32
     call(T, K, N, "bf16", 0, True, True, seed=form)
     call(T, K, N, "f32", 2, True, False, seed=form)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,K,N", [(33, 1040, 2104), (33, 1040, 4104), (20, 528, 20000), (9, 528, 8192), (16, 784, 8200), (8, 528, 8192),
+                                   (17, 16, 264), (12, 48, 8200), (20, 896, 40), (25, 752, 16424)])
+def test_tiles_of_32_tokens(T, K, N, dtype):
+    # one round of 32 x 32 tiles, one of 32 x 64, several (20000, 16424 features); up to 16 tokens with a GPU full of
+    # tiles and without; reductions shorter than the stages, of as many steps, of one more
+    call(T, K, N, dtype, 1, True, True, seed=T)
+    call(T, K, N, dtype, 0, False, False, seed=T + 1, pad=16)
