@@ -458,8 +458,8 @@ rag_status encoder_layer_noalloc(const rag_plan* plan, const void* x, void* y, i
  * int32, exactly; angles in fp64).  T, N and plan->total_tokens are at most 2^24.
  *
  * 8-bit rows: row t of an [rows, d] matrix is int8 q and one fp32 scale, its values
- * q[t][c] * scale[t], with scale[t] = max_c |y[t][c]| / 127 and q = y / scale rounded
- * to nearest even (never -128).  A row whose scale would be subnormal (all zeros
+ * q[t][c] * scale[t], with scale[t] = max_c |y[t][c]| / 127 and q = 127 y / max_c |y|, the
+ * exact quotient rounded to nearest even (never -128).  A row whose scale would be subnormal (all zeros
  * among them) gets scale 0 and q = 0; a row that holds an infinity or a NaN gets
  * scale NaN and q = 0, so that whatever is computed from it is NaN.
  */

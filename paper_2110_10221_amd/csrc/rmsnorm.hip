@@ -1,7 +1,7 @@
 // Root-mean-square norm with the residual's addition, and 8-bit rows: the norm's
 // output, or any matrix, as int8 with one fp32 scale per row.
 //   h = x + residual;  y = gamma * h / sqrt(mean(h^2) + eps)
-//   scale = max |y| / 127;  q = rint(y / scale)
+//   scale = max |y| / 127;  q = rint(127 y / max |y|), the exact quotient's rounding
 // A row stays in registers (16-byte chunks) between its reductions, so it is read once
 // and every output is written once: the operators are bound by HBM bandwidth, and by
 // latency at a few rows.  All of it is fp32; h and y are rounded to the tensor type where
@@ -179,13 +179,29 @@ __global__ __launch_bounds__(256) void k_rmsnorm(NormArgs a) {
     for (int c = 0; c < MAXC; ++c) {
         const int ch = lane + kLanes * c;
         if (ch >= nch) continue;
+        float n[E], edge = 0.f;  // the integers; the largest distance of a quotient from its own
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float z = v[c][e] * mul;
+            n[e] = rintf(z);
+            edge = fmaxf(edge, fabsf(z - n[e]));
+        }
+        // A quotient this near to the middle of two steps may be on its other side, or on it (bf16 rows hold
+        // exact ties by the thousand): mul and the product are each off by half a step of fp32, 2^-16 at most of
+        // 127.  In fp64 z errs by 2^-44 at most, while a quotient of two fp32 values that is not a tie is 2^-34 from
+        // one at least: rounded to a multiple of 2^-40 (by the added 1.5 * 2^12) every tie is one and no other is.
+        if (edge > 0.5f - 0x1p-15f) {
+            const double r = 127.0 / (double)top;
+#pragma unroll
+            for (int e = 0; e < E; ++e) n[e] = (float)rint(fma((double)v[c][e], r, 6144.0) - 6144.0);
+        }
         uint32_t w[E / 4];
 #pragma unroll
         for (int p = 0; p < E / 4; ++p) {
             w[p] = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int i = finite ? (int)rintf(v[c][4 * p + e] * mul) : 0;
+                const int i = finite ? (int)n[4 * p + e] : 0;
                 w[p] |= (uint32_t)(i & 255) << (8 * e);
             }
         }

@@ -163,3 +163,49 @@ def test_another_stream_and_a_replayed_graph():
         rag.packed_rmsnorm(x, g, ref)
         torch.cuda.synchronize()
         assert torch.equal(y, ref)
+
+
+def nearest_even(x):
+    """127 x / max |x| of each row rounded to nearest even, in whole numbers: (q, whether it was a tie)."""
+    top = x.double().abs().amax(1, keepdim=True)
+    unit = torch.floor(torch.log2(top)) - 33  # values above half a step are multiples of 2^unit
+    a, t = (torch.ldexp(v, -unit).trunc().to(torch.int64) for v in (x.double(), top))
+    num = 254 * a.abs() + t  # q = floor(127 a / t + 1 / 2), less one at a tie with an odd one
+    q, tie = num // (2 * t), num % (2 * t) == 0
+    return (q - (tie & (q % 2 == 1)).to(torch.int64)) * torch.sign(a), tie
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_every_tie_of_short_significands_goes_to_even(dtype):
+    # every pair of 8-bit significands (all of bf16's): 102 and 51 are 63.5 steps apart, whatever 127 / 102 is in fp32
+    import paper_2110_10221_amd as rag
+
+    top = torch.arange(128.0, 256.0).repeat_interleave(3)[:, None]
+    x = torch.arange(0.0, 256.0) * torch.tensor([0.5, 1.0, -0.25]).repeat(128)[:, None]
+    x = torch.cat([top, torch.where(x.abs() > top, 0.0, x), torch.zeros(384, 7)], dim=1).to(P.TYPES[dtype])
+    ref, tie = nearest_even(x)
+    assert tie.sum() > 200 and ref[3 * (204 - 128) + 1, 1 + 102] == 64
+    q, s = torch.empty(x.shape, dtype=torch.int8, device="cuda"), torch.empty(384, device="cuda")
+    rag.packed_quantize_i8(x.cuda(), q, s)
+    assert torch.equal(q.cpu().to(torch.int64), ref)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,std", [(2000, 4096, 1.0), (300, 264, 1e-35), (300, 16384, 1e36)])
+def test_integers_are_exact(dtype, T, d, std):
+    import paper_2110_10221_amd as rag
+
+    x = P.normal(T, T, d, dtype=dtype, std=std)
+    q, s = torch.empty(T, d, dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda")
+    rag.packed_quantize_i8(x.cuda(), q, s)
+    assert torch.equal(q.cpu().to(torch.int64), nearest_even(x)[0])
+
+
+def test_integers_of_the_norm_are_exact():
+    # in fp32 y is the unrounded norm, which q is taken from
+    import paper_2110_10221_amd as rag
+
+    x, g = P.normal(1, 500, 1028, dtype="f32").cuda(), P.normal(2, 1028, dtype="f32").cuda()
+    y, q, s = torch.empty_like(x), torch.empty(500, 1028, dtype=torch.int8, device="cuda"), torch.empty(500, device="cuda")
+    rag.packed_rmsnorm(x, g, y, q=q, q_scale=s)
+    assert torch.equal(q.cpu().to(torch.int64), nearest_even(y.cpu())[0])
