@@ -25,8 +25,11 @@
 //           it was moved).  The masks are bits of a word per row and chunk (166 us, 161).
 //   splits  where few rows meet many keys the chunks are dealt to several workgroups
 //           (blockIdx.y), whose (reference, sum, output) states a second launch joins.
-// bf16 rounds the unnormalised exponentials to bf16 for the P V product (a relative 2^-8 at most
-// of each of many terms, beside 2^-8 of the stored result) and nothing else; fp32
+// Nothing is rounded but the result.  In bf16 the P V product takes each exponential as two bf16
+// values, its rounding and the rest (2^-16 of it is lost): the result is 1.65e-3 from the exact one
+// by its norm, its own rounding, where one value gives 2.29e-3 (six prompts of 1500 to 8192 tokens,
+// window 1024, 16/4 heads, 145 us with one, 186 with two; two of 8192, all visible, 16/8 heads, 436 and 581; 32 single
+// tokens 31.1 either way, they wait for memory).  fp32
 // products round nothing; they run on v_mfma_f32_16x16x4f32, 16 keys (4 for P V) by 16 rows at a time, and only
 // those that any row sees: a window of 96 is 111 keys to 16 rows, to 32 x 32 blocks it was 160 (batch 32 of
 // 16 to 512 tokens, 8 heads: 50.9 us on those, 46.5; 64 single tokens, caches to 2048, 8 heads 87, 79; six prompts
@@ -431,13 +434,21 @@ void k_attention_window(WinArgs a) {
             __builtin_amdgcn_s_setprio(1);  // (matrix instructions of one wave beside the others' vector work)
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                u32x4 pw;
+                u32x4 high, low;  // an exponential as two bf16
 #pragma unroll
-                for (int e = 0; e < 4; ++e) pw[e] = pack_bf16x2(sc[0][8 * t + 2 * e], sc[0][8 * t + 2 * e + 1]);
+                for (int e = 0; e < 4; ++e) {
+                    const float p0 = sc[0][8 * t + 2 * e], p1 = sc[0][8 * t + 2 * e + 1];
+                    high[e] = pack_bf16x2(p0, p1);
+                    low[e] = pack_bf16x2(p0 - lo_bf16(high[e]), p1 - hi_bf16(high[e]));
+                }
+                const auto multiply = [&](const u32x4& p) {
 #pragma unroll
-                for (int cb = 0; cb < 2; ++cb)
-                    oacc[0][cb] = mfma32x32x16(as_bf16x8(u32x4{tr[t][cb][0][0], tr[t][cb][0][1], tr[t][cb][1][0], tr[t][cb][1][1]}),
-                                               as_bf16x8(pw), oacc[0][cb]);
+                    for (int cb = 0; cb < 2; ++cb)
+                        oacc[0][cb] = mfma32x32x16(as_bf16x8(u32x4{tr[t][cb][0][0], tr[t][cb][0][1], tr[t][cb][1][0], tr[t][cb][1][1]}),
+                                                   as_bf16x8(p), oacc[0][cb]);
+                };
+                multiply(high);
+                multiply(low);
             }
             __builtin_amdgcn_s_setprio(0);
         } else {

@@ -445,3 +445,24 @@ def test_hidden_values_in_groups_of_four(bad):
     cols = cols.repeat_interleave(H // KV, 0).reshape(-1)  # a query head's channels are its key head's
     assert ok[~sees].all() and ok[sees][:, ~cols].all()
     assert not torch.isfinite(out.cpu().float()[sees][:, cols]).any()
+
+
+@pytest.mark.parametrize("L,kv_len,heads,kv_heads,window", [
+    ([200, 65], None, 2, 2, 100), ([200, 65], None, 8, 2, ALL), ([1, 1, 2], [700, 33, 64], 8, 2, ALL), ([1], [5000], 4, 1, ALL)])
+def test_exponentials_are_not_rounded_to_the_type(L, kv_len, heads, kv_heads, window):
+    # plain64's fp32 tolerance, 2^-16 of each exponential (a half step of bf16, twice) and the half step of the result
+    import paper_2110_10221_amd as rag
+
+    n = kv_len or L
+    first, T, rows = np.concatenate([[0], np.cumsum(n)[:-1]]).tolist(), sum(L), sum(n)
+    q, k, v = P.normal(1, T, heads * 64, std=2.0), P.normal(2, rows, kv_heads * 64), P.normal(3, rows, kv_heads * 64)
+    plan, out = make_plan(L, heads), torch.empty(T, heads * 64, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(rag.ragged_attention_window_workspace(plan, max(n), window, 2, kv_heads), dtype=torch.uint8, device="cuda")
+    if kv_len:
+        rag.ragged_attention_window_cached(plan, q.cuda(), k.cuda(), v.cuda(), torch.tensor(first).cuda(),
+                                           torch.tensor(n, dtype=torch.int32).cuda(), max(n), out, 0.125, window, 2, kv_heads, workspace=ws)
+    else:
+        rag.ragged_attention_window(plan, q.cuda(), k.cuda(), v.cuda(), out, 0.125, window, 2, kv_heads, workspace=ws)
+    ref, mag, bound, count = P.window_attention(L, heads, kv_heads, q, k, v, first, n, window, 2, 0.125)
+    tol = P.window_tolerance("f32", ref, mag, bound, count) + 2.0 ** -16 * mag + P.HALF["bf16"] * ref.abs()
+    assert ((out.cpu().double() - ref).abs() <= tol).all()
