@@ -26,6 +26,15 @@ __device__ __forceinline__ int stream_item(int bid, int nb) {  // nb: a multiple
 
 __device__ __forceinline__ void attn_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// A query's elements times a scale of zero: zero, or NaN where they are not finite.
+__device__ __forceinline__ u32x4 zero_times_bf16(const u32x4& v) {
+    u32x4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        r[i] = ((v[i] & 0x7f80u) == 0x7f80u ? 0x7fffu : 0u) | ((v[i] & 0x7f800000u) == 0x7f800000u ? 0x7fff0000u : 0u);
+    return r;
+}
+
 // Combine a value with the one held by the lane 32 apart (the other half of
 // the same query row): v_permlane32_swap hands each half the other's value.
 __device__ __forceinline__ float max_xor32(float v) {

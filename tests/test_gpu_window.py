@@ -466,3 +466,28 @@ def test_exponentials_are_not_rounded_to_the_type(L, kv_len, heads, kv_heads, wi
     ref, mag, bound, count = P.window_attention(L, heads, kv_heads, q, k, v, first, n, window, 2, 0.125)
     tol = P.window_tolerance("f32", ref, mag, bound, count) + 2.0 ** -16 * mag + P.HALF["bf16"] * ref.abs()
     assert ((out.cpu().double() - ref).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.0, 1e-36, -1e-35])
+def test_small_scales_of_large_products(dtype, scale):
+    # products of about 1e35: uniform weights at a scale of zero, ordinary scores at the others
+    L, H = [70, 33, 1], 2
+    q, k = (P.normal(s, sum(L), H * 64, dtype=dtype, std=1e17) for s in (1, 2))
+    v = P.normal(3, sum(L), H * 64, dtype=dtype)
+    packed(L, H, H, 40, 2, dtype, scale, qkv=(q, k, v))
+    packed(L, H, H, ALL, 0, dtype, scale, qkv=(q, k, v))
+    cached([1, 3], [90, 33], H, H, 40, 2, dtype, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_scale_of_zero_keeps_what_is_not_finite(dtype, bad):
+    import paper_2110_10221_amd as rag
+
+    q, k, v = (P.normal(s, 50, 128, dtype=dtype) for s in range(3))
+    q[20, 64 + 7] = bad  # token 20, head 1
+    plan, out = make_plan([50], 2), torch.empty(50, 128, dtype=q.dtype, device="cuda")
+    rag.ragged_attention_window(plan, q.cuda(), k.cuda(), v.cuda(), out, 0.0, 10, 1)
+    nan = torch.isnan(out.cpu().float())
+    assert nan[20, 64:].all() and nan.sum() == 64
