@@ -26,13 +26,10 @@ __device__ __forceinline__ int stream_item(int bid, int nb) {  // nb: a multiple
 
 __device__ __forceinline__ void attn_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// A query's elements times a scale of zero: zero, or NaN where they are not finite.
-__device__ __forceinline__ u32x4 zero_times_bf16(const u32x4& v) {
-    u32x4 r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        r[i] = ((v[i] & 0x7f80u) == 0x7f80u ? 0x7fffu : 0u) | ((v[i] & 0x7f800000u) == 0x7f800000u ? 0x7fff0000u : 0u);
-    return r;
+// The magnitude of the factor that makes powers of two of scores.  A factor of zero would turn hidden keys' -inf
+// into NaN; the smallest fp32 value in its place leaves every exponential 1: times the largest score it is 5e-7.
+__device__ __forceinline__ float softmax_factor(float scale) {
+    return scale == 0.f ? 0x1p-149f : fabsf(scale) * 1.4426950408889634f;
 }
 
 // Combine a value with the one held by the lane 32 apart (the other half of

@@ -134,8 +134,7 @@ void k_attention_window(WinArgs a) {
     // score r is key 8 (r / 4) + 4 part + r % 4 in bf16 and 16 (r / 4) + 4 (r % 4) + part in fp32.
     constexpr int RB = BF16 ? 1 : 2, LR = kWinBlock / RB, NS = 16 / RB;
     const int lrow = lane % LR, part = lane / LR;
-    // (a zero scale would turn hidden keys' -inf into NaN: the query is made zero in its place)
-    const float zs = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.4426950408889634f;
+    const float zs = softmax_factor(a.scale);
     const bool flip = a.scale < 0.f;
     const int G = a.group;
     // LDS addresses of the transposed V reads in stage 0, key step 0: within 16 lanes, lane 4 e + q
@@ -247,19 +246,6 @@ void k_attention_window(WinArgs a) {
             qf[b][u] = active ? *reinterpret_cast<const u32x4*>(qrow + 16 * u + (BF16 ? 8 : 4) * part) : u32x4{0u, 0u, 0u, 0u};
             if (flip) qf[b][u] ^= BF16 ? 0x80008000u : 0x80000000u;
         }
-    }
-    if (a.scale == 0.f) {
-#pragma unroll
-        for (int b = 0; b < RB; ++b)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                if constexpr (BF16) {
-                    qf[b][u] = zero_times_bf16(qf[b][u]);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) qf[b][u][e] = (qf[b][u][e] & 0x7f800000u) == 0x7f800000u ? 0x7fffffffu : 0u;
-                }
-            }
     }
     float m[RB], lsum[RB];
 #pragma unroll
