@@ -370,3 +370,35 @@ def test_fused_attention_split_keys_reference_raised(step):
     print(f"split-key attention, rising keys {step}", flush=True)
     q, k, v = rising_keys(L, H, step, seed=int(step))
     _fused_close(_fused(L, H, q, k, v, 0.125), L, H, q, k, v, 0.125)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("scale", [0.0, 1e-36, -1e-35])
+def test_fused_attention_small_scales_of_large_products(scale, causal):
+    # products of about 1e35: uniform weights at a scale of zero, ordinary scores at the others.  In half steps: a
+    # score is 64 roundings of at most `bound` and its scaling, an exponential errs by that and 2, sums by one per key
+    # and a few rescalings; every exponential is rounded to bf16 (2^-8), and the result is.
+    import torch
+
+    import paper_2110_10221_amd as rag
+
+    g = torch.Generator().manual_seed(5)
+    L, H = [70, 33, 1, 700], 2
+    T = sum(L)
+    q, k, v = ((torch.randn(T, H * 64, generator=g) * s).to(torch.bfloat16) for s in (1e17, 1e17, 1.0))
+    plan = rag.Plan(torch.tensor(L, dtype=torch.int32).cuda(), T, max(L), H)
+    rag.ragged_offsets(plan)
+    out = torch.empty(T, H * 64, dtype=torch.bfloat16, device="cuda")
+    (rag.ragged_attention_causal if causal else rag.ragged_attention)(plan, q.cuda(), k.cuda(), v.cuda(), out, scale)
+    t0 = 0
+    for n in L:
+        for h in range(H):
+            at = slice(t0, t0 + n), slice(64 * h, 64 * h + 64)
+            qq, kk, vv = (a[at].double() for a in (q, k, v))
+            hidden = torch.ones(n, n).triu(1).bool() if causal else torch.zeros(n, n).bool()
+            p = torch.softmax((qq @ kk.t() * scale).masked_fill(hidden, float("-inf")), 1)
+            bound = (qq.abs() @ kk.abs().t() * abs(scale)).amax(1, keepdim=True)
+            ref = p @ vv
+            tol = p @ vv.abs() * (2 * 2.0 ** -24 * (67 * bound + n + 8) + 2.0 ** -8) + 2.0 ** -8 * ref.abs()
+            assert ((out[at].cpu().double() - ref).abs() <= tol).all()
+        t0 += n
