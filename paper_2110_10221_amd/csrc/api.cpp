@@ -610,7 +610,7 @@ rag_status ragged_trmm(const void* l, int32_t ldl, const void* b, int32_t ldb, v
 
 namespace {
 
-constexpr int32_t kMaxRows = 1 << 24;  // rows: a launch holds up to 256 threads for each, 2^32 at most
+constexpr int32_t kMaxRows = 1 << 24;  // rows
 constexpr int32_t kMaxKeys = 1 << 30;  // keys of a sequence: position arithmetic stays in 32 bits
 
 // Rows read and written in 16-byte chunks in either type.

@@ -6,6 +6,7 @@
 // and every output is written once: the operators are bound by HBM bandwidth, and by
 // latency at a few rows.  All of it is fp32; h and y are rounded to the tensor type where
 // they are stored and nowhere else (the 8-bit rows come from the unrounded y).
+#include <algorithm>
 #include <cfloat>
 
 #include "device_common.h"
@@ -83,13 +84,17 @@ __device__ __forceinline__ float row_reduce(float v, float* slots, Op op) {
     return v;
 }
 
+// Rows of a launch in x where each takes a workgroup, the rest in y: 2^24 workgroups of 256 threads in x would pass
+// the 2^32 - 1 threads that a dimension can have.
+constexpr int kGridRows = 1 << 20;
+
 // WPR waves per row (1: four rows per workgroup; 4: one), at most MAXC chunks per lane.
 template <bool BF16, bool NORM, int WPR, int MAXC>
 __global__ __launch_bounds__(256) void k_rmsnorm(NormArgs a) {
     using IO = RowChunk<BF16>;
     constexpr int E = IO::kPer, kLanes = WPR * kWave;
     __shared__ float slots[4];
-    const int row = WPR == 1 ? blockIdx.x * 4 + uni(threadIdx.x / kWave) : blockIdx.x;
+    const int row = WPR == 1 ? blockIdx.x * 4 + uni(threadIdx.x / kWave) : blockIdx.y * kGridRows + blockIdx.x;
     if (row >= a.T) return;  // (a whole workgroup, or whole waves that share nothing)
     const int lane = threadIdx.x % kLanes, nch = a.d / E;
     const auto add = [](float p, float q) { return p + q; };
@@ -216,19 +221,19 @@ template <bool BF16, bool NORM>
 hipError_t launch_rows(const NormArgs& a, hipStream_t s) {
     constexpr int E = RowChunk<BF16>::kPer;
     const int nch = a.d / E;
-    const dim3 block(256);
+    const dim3 block(256), rows(std::min(a.T, kGridRows), (a.T + kGridRows - 1) / kGridRows);
     // One wave per row up to two chunks a lane, four waves from there on, at any number of rows (us, one and
     // four; bf16 with residual, sum and 8 bits): d 512, 8 and 70312 rows 2.9, 3.3 and 39.7, 82.8; d 1024,
     // 35156 rows 38.0, 50.6; d 2048, 8 and 17578 rows 4.2, 3.4 and 38.9, 39.5; d 4096 6.0, 3.8
     // and 40.8, 38.6.
     if (nch <= kWave) hipLaunchKernelGGL((k_rmsnorm<BF16, NORM, 1, 1>), dim3((a.T + 3) / 4), block, 0, s, a);
     else if (nch <= 2 * kWave) hipLaunchKernelGGL((k_rmsnorm<BF16, NORM, 1, 2>), dim3((a.T + 3) / 4), block, 0, s, a);
-    else if (nch <= 4 * kWave) hipLaunchKernelGGL((k_rmsnorm<BF16, NORM, 4, 1>), dim3(a.T), block, 0, s, a);
-    else if (nch <= 8 * kWave) hipLaunchKernelGGL((k_rmsnorm<BF16, NORM, 4, 2>), dim3(a.T), block, 0, s, a);
-    else if (nch <= 16 * kWave) hipLaunchKernelGGL((k_rmsnorm<BF16, NORM, 4, 4>), dim3(a.T), block, 0, s, a);
-    else if (nch <= 32 * kWave) hipLaunchKernelGGL((k_rmsnorm<BF16, NORM, 4, 8>), dim3(a.T), block, 0, s, a);
+    else if (nch <= 4 * kWave) hipLaunchKernelGGL((k_rmsnorm<BF16, NORM, 4, 1>), rows, block, 0, s, a);
+    else if (nch <= 8 * kWave) hipLaunchKernelGGL((k_rmsnorm<BF16, NORM, 4, 2>), rows, block, 0, s, a);
+    else if (nch <= 16 * kWave) hipLaunchKernelGGL((k_rmsnorm<BF16, NORM, 4, 4>), rows, block, 0, s, a);
+    else if (nch <= 32 * kWave) hipLaunchKernelGGL((k_rmsnorm<BF16, NORM, 4, 8>), rows, block, 0, s, a);
     else if constexpr (!BF16)  // (bf16 rows end there)
-        hipLaunchKernelGGL((k_rmsnorm<BF16, NORM, 4, 16>), dim3(a.T), block, 0, s, a);
+        hipLaunchKernelGGL((k_rmsnorm<BF16, NORM, 4, 16>), rows, block, 0, s, a);
     return hipGetLastError();
 }
 

@@ -209,3 +209,22 @@ def test_integers_of_the_norm_are_exact():
     y, q, s = torch.empty_like(x), torch.empty(500, 1028, dtype=torch.int8, device="cuda"), torch.empty(500, device="cuda")
     rag.packed_rmsnorm(x, g, y, q=q, q_scale=s)
     assert torch.equal(q.cpu().to(torch.int64), nearest_even(y.cpu())[0])
+
+
+def test_the_largest_number_of_rows():
+    # 2^24 rows of a workgroup each (43 GB): 2^32 threads
+    import paper_2110_10221_amd as rag
+
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB of free memory")
+    T, d = 2 ** 24, 516
+    x = torch.zeros(T, d, device="cuda")
+    x[:, 0] = 127.0
+    x[:, d - 1] = torch.arange(T, device="cuda") % 127
+    q, s = torch.empty(T, d, dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda")
+    rag.packed_quantize_i8(x, q, s)
+    assert (s == 1.0).all() and (q[:, 0] == 127).all() and (q[:, 1:d - 1] == 0).all()
+    assert torch.equal(q[:, d - 1].long(), torch.arange(T, device="cuda") % 127)
+    del x, q, s
+    torch.cuda.empty_cache()
