@@ -309,11 +309,16 @@ __device__ __forceinline__ void i8_tile(const I8Args& a, int m0, int n0, int8_t*
     }
 }
 
+// Tiles of a launch in x, the rest in y: with 512 threads each 2^31 of the 2^32 - 1 that a dimension can have.
+constexpr int kGridTiles = 1 << 22;
+
 template <class C, bool BF16, int ACT>
 __global__ __launch_bounds__(C::kThreads, C::kWavesPerSimd) void k_linear_i8(I8Args a, int tiles_m, int tiles_n) {
     extern __shared__ __attribute__((aligned(16))) int8_t smem_i8[];
+    const int bid = blockIdx.y * kGridTiles + blockIdx.x;
+    if (bid >= tiles_m * tiles_n) return;
     int tm, tn;
-    tile_coords(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, tm, tn);
+    tile_coords(bid, tiles_m * tiles_n, tiles_m, tiles_n, tm, tn);
     i8_tile<C, BF16, ACT>(a, tm * C::TM, tn * C::TN, smem_i8);
 }
 
@@ -335,7 +340,9 @@ hipError_t launch_tiles(const I8Args& a, hipStream_t s) {
     }
     const int64_t tiles_m = ((int64_t)a.T + C::TM - 1) / C::TM, tiles_n = ((int64_t)a.N + C::TN - 1) / C::TN;
     if (tiles_m * tiles_n > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(f, dim3((unsigned)(tiles_m * tiles_n)), dim3(C::kThreads), C::kLds, s, a, (int)tiles_m, (int)tiles_n);
+    const int64_t tiles = tiles_m * tiles_n;
+    const dim3 grid((unsigned)std::min<int64_t>(tiles, kGridTiles), (unsigned)((tiles + kGridTiles - 1) / kGridTiles));
+    hipLaunchKernelGGL(f, grid, dim3(C::kThreads), C::kLds, s, a, (int)tiles_m, (int)tiles_n);
     return hipGetLastError();
 }
 

@@ -179,3 +179,23 @@ def test_tiles_of_32_tokens(T, K, N, dtype):
     # tiles and without; reductions shorter than the stages, of as many steps, of one more
     call(T, K, N, dtype, 1, True, True, seed=T)
     call(T, K, N, dtype, 0, False, False, seed=T + 1, pad=16)
+
+
+def test_the_largest_outputs():
+    # 2^36 features of tokens (137 GB) in 2^24 tiles of 256 threads
+    import paper_2110_10221_amd as rag
+
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 200 << 30:
+        pytest.skip("needs 200 GB of free memory")
+    T, K, N = 4096, 16, 2 ** 24
+    a, b = torch.arange(T, device="cuda") % 5 + 1, torch.arange(N, device="cuda") % 7 + 1
+    x, w = (v.to(torch.int8)[:, None].expand(-1, K).contiguous() for v in (a, b))
+    y = torch.zeros(T, N, dtype=torch.bfloat16, device="cuda")
+    rag.packed_linear_i8(x, torch.ones(T, device="cuda"), w, torch.ones(N, device="cuda"), y)
+    for i in range(5):
+        row = (16 * (i + 1) * b).to(torch.bfloat16)  # (whole numbers of at most eight bits)
+        for t in range(i, T, 1000):
+            assert (y[t:t + 1000:5] == row).all()
+    del x, w, y
+    torch.cuda.empty_cache()
