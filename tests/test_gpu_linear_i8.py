@@ -199,3 +199,23 @@ def test_the_largest_outputs():
             assert (y[t:t + 1000:5] == row).all()
     del x, w, y
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [3, 40, 300])
+def test_scales_near_the_range(T, dtype):
+    # sum * x_scale passes fp32's range, sum * x_scale * w_scale does not; a sum of zero stays zero
+    import paper_2110_10221_amd as rag
+
+    K, N = 256, 264
+    x, w, b = int8(1, T, K), int8(2, N, K), P.normal(3, N, dtype=dtype)
+    x[1] = 0
+    xs, ws = scales(4, T) * 2e36, scales(5, N) * 1e-10
+    xs[::2] *= -1e-30
+    w[5], ws[5] = 0, 3e38
+    y = torch.empty(T, N, dtype=P.TYPES[dtype], device="cuda")
+    rag.packed_linear_i8(x.cuda(), xs.cuda(), w.cuda(), ws.cuda(), y, b.cuda())
+    lin = (x.double() @ w.double().t()) * xs.double()[:, None] * ws.double()
+    ref = lin + b.double()
+    tol = F32 * (4 * lin.abs() + b.double().abs() + 2 * ref.abs()) + P.HALF[dtype] * ref.abs()
+    assert ((y.cpu().double() - ref).abs() <= tol).all()
