@@ -12,6 +12,7 @@ Function names match the C interface in include/ragged.h.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 
 import torch
@@ -330,7 +331,20 @@ def _launch_stream(stream, dev, plan=None):
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
-_I32_MAX = 2 ** 31 - 1  # (ctypes would wrap a larger window; no position passes it)
+_I32_MAX = 2 ** 31 - 1
+
+
+def _i32(name, n):
+    """The integer itself: ctypes would wrap one past 32 bits."""
+    n = operator.index(n)
+    if not -_I32_MAX - 1 <= n <= _I32_MAX:
+        raise ValueError(f"{name} {n} does not fit into 32 bits")
+    return n
+
+
+def _bound(name, n):
+    """A window or a bound: past 2^31 - 1, which no position passes, the same as that."""
+    return _I32_MAX if n > _I32_MAX else _i32(name, n)
 
 
 def _sizes(*n):
@@ -388,14 +402,15 @@ def _checked_linear_i8(x, x_scale, w, w_scale, y, bias, residual, act, stream):
         raise ValueError("w must be contiguous")
     return _c_linear_i8(x.data_ptr(), _mat("x", x, (T, K), torch.int8, dev), _vec("x_scale", x_scale, T, torch.float32, dev),
                         w.data_ptr(), _vec("w_scale", w_scale, N, torch.float32, dev), _vec("bias", bias, N, dt, dev),
-                        _addr(residual), _mat("residual", residual, (T, N), dt, dev), act, y.data_ptr(),
+                        _addr(residual), _mat("residual", residual, (T, N), dt, dev), _i32("act", act), y.data_ptr(),
                         _mat("y", y, (T, N), dt, dev), T, K, N, _CODES[dt], _launch_stream(stream, dev))
 
 
 def rotary_frequencies(rot_dim, base=10000.0, scaling=RAG_ROTARY_PLAIN, factor=1.0, orig_len=0, beta_fast=32.0,
                        beta_slow=1.0):
     """(angle per position of each of rot_dim / 2 pairs, a float64 tensor on the CPU; amplitude)."""
-    f = torch.empty(max(rot_dim // 2, 1), dtype=torch.float64)
+    rot_dim, scaling, orig_len = _i32("rot_dim", rot_dim), _i32("scaling", scaling), _i32("orig_len", orig_len)
+    f = torch.empty(min(max(rot_dim // 2, 1), RAG_ROTARY_MAX_DIM), dtype=torch.float64)  # (longer ones are refused)
     a = _f64()
     _check("rotary_frequencies", _c_rotary_frequencies(rot_dim, base, scaling, factor, orig_len, beta_fast, beta_slow,
                                                        _ptr(f), ctypes.addressof(a)))
@@ -412,6 +427,7 @@ def packed_rotary(plan: Plan, x, y, inv_freq, heads, head_dim=RAG_HEAD_DIM, layo
         dt, dev, n = x.dtype, x.get_device(), inv_freq.numel()
         shape = (plan.total_tokens, heads * head_dim)
         _sizes(2 * n)
+        heads, head_dim, layout = _i32("heads", heads), _i32("head_dim", head_dim), _i32("layout", layout)
         st = _c_rotary(plan.ref(), x.data_ptr(), _mat("x", x, shape, dt, dev), y.data_ptr(), _mat("y", y, shape, dt, dev), heads,
                        head_dim, 2 * n, layout | (RAG_ROTARY_INVERSE if inverse else 0),
                        _vec("inv_freq", inv_freq, n, torch.float64, dev), amplitude,
@@ -423,9 +439,9 @@ def packed_rotary(plan: Plan, x, y, inv_freq, heads, head_dim=RAG_HEAD_DIM, layo
 def ragged_attention_window_workspace(plan: Plan, max_kv_len, window, sinks=0, kv_heads=None, dtype=torch.bfloat16):
     """Workspace bytes of the two calls below (max_kv_len: plan.max_len for the first; may be 0)."""
     n = ctypes.c_size_t()
-    _check("ragged_attention_window_workspace", _c_window_ws(plan.ref(), min(max_kv_len, _I32_MAX), kv_heads or plan.heads,
-                                                             min(window, _I32_MAX), min(sinks, _I32_MAX), _CODES[dtype],
-                                                             ctypes.byref(n)))
+    _check("ragged_attention_window_workspace",
+           _c_window_ws(plan.ref(), _bound("max_kv_len", max_kv_len), _i32("kv_heads", kv_heads or plan.heads),
+                        _bound("window", window), _bound("sinks", sinks), _CODES[dtype], ctypes.byref(n)))
     return n.value
 
 
@@ -447,10 +463,10 @@ def ragged_attention_window(plan: Plan, q, k, v, out, scale, window, sinks=0, kv
     k and v hold kv_heads (default: all) heads, each shared by plan.heads / kv_heads query heads."""
     st = _fast.ragged_attention_window(plan, q, k, v, out, scale, window, sinks, kv_heads, head_dim, workspace, stream)
     if st is None:
-        kvh = kv_heads or plan.heads
+        kvh, head_dim = _i32("kv_heads", kv_heads or plan.heads), _i32("head_dim", head_dim)
         code, dev, ld, ws, n = _window_operands(plan, q, k, v, out, plan.total_tokens, kvh, head_dim, workspace)
         st = _c_window(plan.ref(), q.data_ptr(), ld[0], k.data_ptr(), ld[1], v.data_ptr(), ld[2], kvh, head_dim, scale,
-                       min(window, _I32_MAX), min(sinks, _I32_MAX), out.data_ptr(), ld[3], ws, n, code,
+                       _bound("window", window), _bound("sinks", sinks), out.data_ptr(), ld[3], ws, n, code,
                        _launch_stream(stream, dev, plan))
     if st:
         _check("ragged_attention_window", st)
@@ -463,12 +479,12 @@ def ragged_attention_window_cached(plan: Plan, q, k, v, kv_first, kv_len, max_kv
     st = _fast.ragged_attention_window_cached(plan, q, k, v, kv_first, kv_len, max_kv_len, out, scale, window, sinks, kv_heads,
                                               head_dim, workspace, stream)
     if st is None:
-        kvh, rows = kv_heads or plan.heads, k.shape[0]
+        kvh, head_dim, rows = _i32("kv_heads", kv_heads or plan.heads), _i32("head_dim", head_dim), k.shape[0]
         code, dev, ld, ws, n = _window_operands(plan, q, k, v, out, rows, kvh, head_dim, workspace)
         st = _c_window_cached(plan.ref(), q.data_ptr(), ld[0], k.data_ptr(), ld[1], v.data_ptr(), ld[2], rows,
                               _vec("kv_first", kv_first, plan.batch, torch.int64, dev),
-                              _vec("kv_len", kv_len, plan.batch, torch.int32, dev), min(max_kv_len, _I32_MAX), kvh,
-                              head_dim, scale, min(window, _I32_MAX), min(sinks, _I32_MAX), out.data_ptr(), ld[3], ws, n, code,
+                              _vec("kv_len", kv_len, plan.batch, torch.int32, dev), _bound("max_kv_len", max_kv_len), kvh,
+                              head_dim, scale, _bound("window", window), _bound("sinks", sinks), out.data_ptr(), ld[3], ws, n, code,
                               _launch_stream(stream, dev, plan))
     if st:
         _check("ragged_attention_window_cached", st)

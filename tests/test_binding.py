@@ -129,3 +129,63 @@ def test_refusals_of_the_library_reach_the_caller():
         rag.packed_rmsnorm(args[0], args[1], args[2][:, :32])
     with pytest.raises(ValueError):
         rag.packed_rmsnorm(args[0].cpu(), args[1].cpu(), args[2].cpu())
+
+
+@pytest.mark.parametrize("n", [64 - 2 ** 32, -2 ** 40, -2 ** 31 - 1])
+def test_integers_below_32_bits_are_refused(n):
+    # (ctypes would wrap them: 64 - 2^32 to a window of 64); CPU tensors, so that nothing could launch
+    import types
+
+    import paper_2110_10221_amd as rag
+
+    x, q, v = torch.zeros(4, 64), torch.zeros(4, 64, dtype=torch.int8), torch.zeros(4)
+    plan = types.SimpleNamespace(total_tokens=4, heads=1, batch=1, max_len=4, ref=lambda: None, status=torch.zeros(4))
+    first, length = torch.zeros(1, dtype=torch.int64), torch.ones(1, dtype=torch.int32)
+    window = dict(window=3, sinks=1)
+    for name in window:
+        with pytest.raises(ValueError, match="32 bits"):
+            rag.ragged_attention_window(plan, x, x, x, x, 0.1, **{**window, name: n})
+        with pytest.raises(ValueError, match="32 bits"):
+            rag.ragged_attention_window_cached(plan, x, x, x, first, length, 4, x, 0.1, **{**window, name: n})
+        with pytest.raises(ValueError, match="32 bits"):
+            rag.ragged_attention_window_workspace(plan, 4, **{**window, name: n})
+    with pytest.raises(ValueError, match="32 bits"):
+        rag.ragged_attention_window_cached(plan, x, x, x, first, length, n, x, 0.1, 3)
+    with pytest.raises(ValueError, match="32 bits"):
+        rag.ragged_attention_window_workspace(plan, n, 3)
+    with pytest.raises(ValueError, match="32 bits"):
+        rag.packed_rotary(plan, x, x, torch.zeros(4, dtype=torch.float64), 1, 64, layout=n)
+    with pytest.raises(ValueError, match="32 bits"):
+        rag.packed_linear_i8(q, v, q[:4], v[:4], torch.zeros(4, 4), act=n)
+    for name in ("rot_dim", "scaling", "orig_len"):
+        with pytest.raises(ValueError, match="32 bits"):
+            rag.rotary_frequencies(**{"rot_dim": 64, name: n})
+
+
+@pytest.mark.parametrize("n", [2 ** 31, 2 ** 32, 2 ** 32 + 1])
+def test_integers_above_32_bits_are_refused_where_nothing_is_open(n):
+    import types
+
+    import paper_2110_10221_amd as rag
+
+    x, q, v = torch.zeros(4, 64), torch.zeros(4, 64, dtype=torch.int8), torch.zeros(4)
+    plan = types.SimpleNamespace(total_tokens=4, heads=1, batch=1, max_len=4, ref=lambda: None, status=torch.zeros(4))
+    with pytest.raises(ValueError, match="32 bits"):
+        rag.packed_linear_i8(q, v, q[:4], v[:4], torch.zeros(4, 4), act=n)
+    with pytest.raises(ValueError, match="32 bits"):
+        rag.packed_rotary(plan, x, x, torch.zeros(4, dtype=torch.float64), 1, 64, layout=n)
+    for name in ("rot_dim", "scaling", "orig_len"):
+        with pytest.raises(ValueError, match="32 bits"):
+            rag.rotary_frequencies(**{"rot_dim": 64, name: n})
+
+
+@pytest.mark.gpu
+def test_open_windows_may_be_any_number_above():
+    import paper_2110_10221_amd as rag
+
+    args, _ = calls()["ragged_attention_window"]
+    outs = []
+    for window in (2 ** 31 - 1, 2 ** 40, float("inf")):
+        rag.ragged_attention_window(*args[:5], 0.3, window, 2 ** 40)
+        outs.append(args[4].clone())
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
