@@ -17,6 +17,8 @@ import os
 
 import torch
 
+from ._build import built_for
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libragged.so")
 
@@ -43,8 +45,8 @@ RAG_ROTARY_MAX_DIM = 512
 VGEMM_DATA_BITS = {1: "negative size", 2: "size > RAG_VGEMM_MAX_DIM", 4: "tile_cap exceeded",
                    8: "operand buffer too small", 16: "bf16 needs k % 64 == 0 and n % 8 == 0"}
 
-if not os.path.exists(LIB_PATH) or not os.path.exists(os.path.join(_HERE, "_binding.so")):
-    raise ImportError(f"{LIB_PATH} or _binding.so is missing: build the HIP library first "
+if not os.path.exists(LIB_PATH):
+    raise ImportError(f"{LIB_PATH} is missing: build the HIP library first "
                       "(python paper_2110_10221_amd/_build.py)")
 
 _lib = ctypes.CDLL(LIB_PATH)
@@ -280,10 +282,24 @@ def packed_layernorm(x, gamma, beta, y, eps=1e-5, stream=None):
 # The operators below check types, shapes and devices of what they are given.  A step of single tokens
 # takes as long as its host side, so calls whose arguments are as documented are read, checked and
 # made by _binding.so (packed_rmsnorm of 8 x 1024, call after call: 3.5 us, 6.4 by way of ctypes); it returns None, and
-# launches nothing, for any other call, which then meets the checks written out here.
+# launches nothing, for any other call, which then meets the checks written out here.  It is linked against
+# torch: where it is missing, does not load or was built for another torch or Python, every call goes by way of ctypes.
 
-from . import _binding as _fast  # noqa: E402
 
+class _Unbound:
+    def __getattr__(self, name):
+        return lambda *args: None
+
+
+def _load_fast():
+    try:
+        from . import _binding
+    except ImportError:
+        return _Unbound()
+    return _binding if getattr(_binding, "built_for", None) == built_for() else _Unbound()
+
+
+_fast = _load_fast()
 _fast.bind(torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
            *(ctypes.cast(f, _p).value for f in (_c_rmsnorm, _c_quantize_i8, _c_linear_i8, _c_rotary, _c_window, _c_window_cached)))
 

@@ -50,6 +50,15 @@ def _compile(src: str, defines=(), obj_dir: str = OBJ_DIR, sanitize: bool = Fals
     return obj
 
 
+def built_for() -> str:
+    """What _binding.so depends on; it holds this text of its build."""
+    import sys
+
+    import torch
+
+    return f"torch {torch.__version__}, Python {sys.version_info[0]}.{sys.version_info[1]}"
+
+
 def _build_binding() -> str:
     import sysconfig
 
@@ -58,7 +67,7 @@ def _build_binding() -> str:
     base = os.path.dirname(torch.__file__)
     tmp = BINDING + ".tmp"
     cmd = [shutil.which("g++") or hipcc(), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I", INCLUDE,
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", f'-DRAG_BUILT_FOR="{built_for()}"', "-I", INCLUDE,
            "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(base, "include"),
            os.path.join(CSRC, "binding.cpp"), "-o", tmp,
            "-L" + os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]

@@ -275,5 +275,8 @@ PyMODINIT_FUNC PyInit__binding() {
     name_c = PyUnicode_InternFromString("c");
     name_status = PyUnicode_InternFromString("status");
     name_stream = PyUnicode_InternFromString("cuda_stream");
-    return name_c && name_status && name_stream ? PyModule_Create(&module) : nullptr;
+    if (!name_c || !name_status || !name_stream) return nullptr;
+    PyObject* m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "built_for", RAG_BUILT_FOR) != 0) Py_CLEAR(m);
+    return m;
 }

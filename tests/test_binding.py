@@ -189,3 +189,32 @@ def test_open_windows_may_be_any_number_above():
         rag.ragged_attention_window(*args[:5], 0.3, window, 2 ** 40)
         outs.append(args[4].clone())
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+@pytest.mark.parametrize("what", ["absent", "not a library", "of another torch"])
+def test_the_package_needs_no_compiled_part(what, tmp_path):
+    import subprocess
+    import sys
+
+    package = tmp_path / "paper_2110_10221_amd"
+    package.mkdir()
+    for name in ("__init__.py", "_build.py", "libragged.so"):
+        os.symlink(os.path.join(ROOT, "paper_2110_10221_amd", name), package / name)
+    if what == "not a library":
+        (package / "_binding.so").write_bytes(b"\0" * 100)
+    elif what == "of another torch":
+        (package / "_binding.py").write_text("built_for = 'torch 1.0'\ndef bind(*a):\n    raise SystemError\n")
+    code = ("import torch, paper_2110_10221_amd as rag\n"
+            f"assert rag.__file__.startswith({str(tmp_path)!r})\n"
+            "assert rag._fast.packed_rmsnorm(1, 2) is None and rag.rotary_frequencies(64)[0].numel() == 32\n"
+            "x = torch.zeros(4, 64)\n"
+            "try:\n    rag.packed_rmsnorm(x, x[0], x[:, :8])\n"
+            "except ValueError as e:\n    assert 'y must be' in str(e)\n"
+            "else:\n    raise SystemError('not refused')\n")
+    subprocess.run([sys.executable, "-c", code], cwd=tmp_path, check=True, timeout=100, env={**os.environ, "PYTHONPATH": str(tmp_path)})
+
+
+def test_the_compiled_part_is_used_where_it_fits():
+    import paper_2110_10221_amd as rag
+
+    assert rag._fast.__name__.endswith("_binding") and rag._fast.built_for == rag.built_for()
