@@ -4,8 +4,8 @@
 // cores (v_mfma_i32_16x16x64_i8; K <= 131056 keeps the sums below 2^31) and scales, bias, activation and
 // residual applied in fp32 to the finished sum, which is rounded to the type once.
 //
-// Up to 16 tokens go to a kernel of their own (further down), others to TM x TN tiles, one per
-// workgroup of WM x WN (x WK, over k) waves, of the size that linear_form_i8 picks.  What bounds them:
+// linear_kernel_i8 picks the kernel: one of its own for few tokens (further down), or TM x TN tiles, one
+// per workgroup of WM x WN (x WK, over k) waves.  What bounds them:
 // moving operands from L2 into LDS on the small ones (a 64 x 64 tile takes 16 KB per 0.22 us of a CU),
 // the matrix cores and power on 256 x 256 ones: 8192^3 413 us, 2660 TOPS.  Operands go global -> LDS
 // by bounds-checked direct copies, 128 k (one 128-byte line) of each row per stage, ST stages; the
@@ -446,32 +446,17 @@ hipError_t launch_few(const I8Args& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Tiles of 32 tokens.  Where they are fewer than the CUs each CU runs one at its own copies' latency: 32
-// features if that many tiles still fit one round, and six stages (us with 64 features and four stages, as the other
-// calls run, and so: 32 x 4096 x 4096 11.1, 8.2; 64 x 8192 x 2048 18.3, 12.4; 32 x 1024 x 1024 3.9, 3.8;
-// with 64 features and six 100 x 4096 x 4096 10.7, 8.8; 160 x 1024 x 4096, more tiles than CUs, 5.0, 5.5).
 template <bool BF16, int ACT>
-hipError_t launch_tiles32(const I8Args& a, int cus, hipStream_t s) {
-    const int64_t rows = ((int64_t)a.T + 31) / 32;
-    if (rows * (((int64_t)a.N + 31) / 32) <= cus) return launch_tiles<I8Cfg<32, 32, 1, 1, 2, 6>, BF16, ACT>(a, s);
-    if (rows * (((int64_t)a.N + 63) / 64) <= cus) return launch_tiles<I8Cfg<32, 64, 1, 2, 2, 6>, BF16, ACT>(a, s);
-    return launch_tiles<I8Cfg<32, 64, 1, 2, 2, 4>, BF16, ACT>(a, s);
-}
-
-template <bool BF16, int ACT>
-hipError_t launch_form(const I8Args& a, hipStream_t s) {
+hipError_t launch_kernel(const I8Args& a, hipStream_t s) {
     const int cus = device_cu_count();
-    switch (linear_form_i8(a.T, a.K, a.N, ACT, BF16, cus)) {
-        case 0:
-            // its workgroups read all of x for 16 features each: with more than a few tokens and a GPU full of tiles
-            // those are faster (us at 1, 8 and 16 tokens, and on tiles at any of them: 8192 x 8192 15.5, 16.8, 19.7, and
-            // 15.4; 4096 x 16384 15.3, 17.2, 20.9, and 16.8)
-            if (a.T > 4 && a.N >= 32 * cus) return launch_tiles32<BF16, ACT>(a, cus, s);
-            return launch_few<BF16, ACT>(a, s);
-        case 1: return launch_tiles32<BF16, ACT>(a, cus, s);
-        case 2: return launch_tiles<I8Cfg<64, 64, 2, 2, 1, 3>, BF16, ACT>(a, s);
-        case 3: return launch_tiles<I8Cfg<64, 128, 2, 2, 1, 3>, BF16, ACT>(a, s);
-        case 4: return launch_tiles<I8Cfg<128, 128, 2, 4, 1, 2>, BF16, ACT>(a, s);
+    switch (linear_kernel_i8(a.T, a.K, a.N, ACT, BF16, cus)) {
+        case kI8Few: return launch_few<BF16, ACT>(a, s);
+        case kI8Tiles32x32: return launch_tiles<I8Cfg<32, 32, 1, 1, 2, 6>, BF16, ACT>(a, s);
+        case kI8Tiles32x64Deep: return launch_tiles<I8Cfg<32, 64, 1, 2, 2, 6>, BF16, ACT>(a, s);
+        case kI8Tiles32x64: return launch_tiles<I8Cfg<32, 64, 1, 2, 2, 4>, BF16, ACT>(a, s);
+        case kI8Tiles64x64: return launch_tiles<I8Cfg<64, 64, 2, 2, 1, 3>, BF16, ACT>(a, s);
+        case kI8Tiles64x128: return launch_tiles<I8Cfg<64, 128, 2, 2, 1, 3>, BF16, ACT>(a, s);
+        case kI8Tiles128x128: return launch_tiles<I8Cfg<128, 128, 2, 4, 1, 2>, BF16, ACT>(a, s);
         default: return launch_big<BF16, ACT>(a, cus, s);
     }
 }
@@ -479,25 +464,24 @@ hipError_t launch_form(const I8Args& a, hipStream_t s) {
 template <bool BF16>
 hipError_t launch_type(const I8Args& a, int act, hipStream_t s) {
     switch (act) {
-        case 1: return launch_form<BF16, 1>(a, s);
-        case 2: return launch_form<BF16, 2>(a, s);
-        default: return launch_form<BF16, 0>(a, s);
+        case 1: return launch_kernel<BF16, 1>(a, s);
+        case 2: return launch_kernel<BF16, 2>(a, s);
+        default: return launch_kernel<BF16, 0>(a, s);
     }
 }
 
 }  // namespace
 
-// The form of a call: 0 few tokens, 1 .. 4 the tiles of 32 tokens (two k shares), 64 x 64, 64 x 128
-// and 128 x 128, 5 the 256 x 256 tiles and quarters.  Up to 16 tokens the first one (T = 16, K = N =
-// 4096: 6.7 us, 7.7 on 32 x 64 tiles; T = 32: 8.6 and 7.9).  Above, the smallest of the modelled times
-// in us
+// The form of tiles for a call: 0 few tokens (at most 16), 1 .. 4 tiles of 32 tokens (two k shares), 64 x 64, 64 x 128
+// and 128 x 128, 5 the 256 x 256 tiles and quarters: the smallest of the modelled times in us
 //     start + max(epilogue + nk * alone, rounds * (epilogue + nk * step))
 // nk the 128-k steps, rounds the tiles of the busiest CU, `alone` a step's latency and `step` its
 // share of a busy CU's time, the epilogue longer with an activation or fp32 outputs.  Fitted to
-// 355 shapes (T 17 to 40000, K 256 to 8192, N 64 to 8192, both types, every epilogue), where
-// the choice takes 1.3% more than the fastest form on average and 30% at worst (0.9% and 29% on 355
-// others).  Both sides, us on forms 1 to 5: 2237 x 2048 x 512 fp32 10.6, 10.1, 10.4, 15.3, 13.0;
-// 35475 x 1024 x 4096 GELU 395, 291, 264, 225, 229; 35475 x 4096 x 1024 with residual 336, 225, 190, 168, 140.
+// 355 shapes (T 17 to 40000, K 256 to 8192, N 64 to 8192, both types, every epilogue) with 32 x 64 tiles of
+// four stages as form 1.  On 240 others the kernel that linear_kernel_i8 makes of it takes 1.5% more than the
+// fastest of the seven on average and 25% at worst (up to 400 tokens 1.0%).  Us on forms 1 to 5: 2237 x 2048 x 512 fp32
+// 9.6, 8.9, 9.1, 14.7, 12.2; 35475 x 1024 x 4096 GELU 395, 291, 264, 225, 229; 35475 x 4096 x 1024 with residual
+// 336, 225, 190, 168, 140.
 int linear_form_i8(int64_t T, int64_t K, int64_t N, int act, bool bf16, int64_t cus) {
     if (T <= 16) return 0;
     struct Cost {
@@ -522,6 +506,23 @@ int linear_form_i8(int64_t T, int64_t K, int64_t N, int act, bool bf16, int64_t 
         if (t < best) best = t, form = i + 1;
     }
     return form;
+}
+
+// The kernel of a call.  Figures are us with the weights out of the caches, and in them.
+int linear_kernel_i8(int64_t T, int64_t K, int64_t N, int act, bool bf16, int64_t cus) {
+    const int form = linear_form_i8(T, K, N, act, bf16, cus);
+    if (form > 1) return kI8Tiles64x64 + form - 2;
+    // The few tokens' workgroups read all of x for 16 features each: with more than four tokens and a GPU full of tiles
+    // of 32 those are faster (8192 x 8192 with 1, 8 and 16 tokens 15.0, 14.0; 16.1, 15.1; 19.2, 17.3, and on tiles with any
+    // 14.9, 12.8; 16 x 4096 x 16384 20.4, 17.6 and 16.3, 12.4), with fewer tiles they are not (16 x 4096 x 4096 7.0, 6.6 and
+    // 7.7, 7.6).
+    if (form == 0 && !(T > 4 && N >= 32 * cus)) return kI8Few;
+    // Where the tiles of 32 tokens are fewer than the CUs each CU runs one at its own copies' latency: 32 features if that
+    // many tiles still fit one round, and six stages, else 64 features and four.  On 32 x 32, 32 x 64 with six and with four
+    // stages: 32 x 4096 x 4096 8.1, 10.2, 11.0 (in the caches 7.7, 7.4, 7.2); 64 x 8192 x 2048 12.3, 16.0, 18.2 (12.3, 11.5,
+    // 11.4); 100 x 4096 x 4096 10.1, 8.7, 10.5 (9.3, 8.0, 7.8); 160 x 1024 x 4096, more tiles than CUs, 5.5, 5.6, 5.2 (5.5, 5.7, 5.2).
+    const int64_t rows = (T + 31) / 32;
+    return rows * ((N + 31) / 32) <= cus ? kI8Tiles32x32 : rows * ((N + 63) / 64) <= cus ? kI8Tiles32x64Deep : kI8Tiles32x64;
 }
 
 hipError_t launch_linear_i8(int dtype, const int8_t* x, int ldx, const float* x_scale, const int8_t* w,

@@ -91,8 +91,10 @@ hipError_t launch_rotary(const PlanView& p, int dtype, const void* x, int ldx, v
                          const int32_t* pos_start, hipStream_t s);
 
 // y = act(x_scale w_scale x w^T + bias) + residual on 8-bit rows; dtype is that of bias, residual and y.
-// (linear_form_i8: the tile form it runs, by its sizes)
+// linear_form_i8: the form of tiles that is modelled fastest for its sizes; linear_kernel_i8: the kernel that runs.
+enum { kI8Few, kI8Tiles32x32, kI8Tiles32x64Deep, kI8Tiles32x64, kI8Tiles64x64, kI8Tiles64x128, kI8Tiles128x128, kI8Tiles256x256 };
 int linear_form_i8(int64_t T, int64_t K, int64_t N, int act, bool bf16, int64_t cus);
+int linear_kernel_i8(int64_t T, int64_t K, int64_t N, int act, bool bf16, int64_t cus);
 hipError_t launch_linear_i8(int dtype, const int8_t* x, int ldx, const float* x_scale, const int8_t* w,
                             const float* w_scale, const void* bias, const void* residual, int ldr, int act, void* y,
                             int ldy, int T, int K, int N, hipStream_t s);
