@@ -500,10 +500,12 @@ enum { RAG_ROTARY_HALF = 0,        /* pair i is channels i and i + rot_dim / 2  
 /* Frequencies for contexts `factor` times longer than trained on. */
 enum { RAG_ROTARY_PLAIN = 0,  /* base^(-2i / rot_dim)                                          */
        RAG_ROTARY_LINEAR = 1, /* those over factor (positions interpolated)                    */
-       RAG_ROTARY_NTK = 2,    /* base * factor^(rot_dim / (rot_dim - 2)) as the base           */
-       RAG_ROTARY_YARN = 3 }; /* Peng et al., YaRN: pairs that turn more than beta_fast times over
-                                 orig_len positions keep their frequency, below beta_slow it is
-                                 divided by factor, a ramp between; amplitude 0.1 ln(factor) + 1 */
+       RAG_ROTARY_NTK = 2,    /* base * factor^(rot_dim / (rot_dim - 2)) as the base (rot_dim 2: base) */
+       RAG_ROTARY_YARN = 3 }; /* Peng et al., YaRN: with p(beta) the pair, as a real number, that turns beta
+                                 times over orig_len positions, pairs up to max(floor p(beta_fast), 0)
+                                 keep their frequency (pair 0 always), from min(ceil p(beta_slow),
+                                 rot_dim - 1) on it is divided by factor, between them the two are mixed
+                                 along a ramp; amplitude 0.1 ln(factor) + 1 */
 
 /*
  * (host only)  inv_freq[rot_dim / 2] (host) and amplitude (host) of one of the rules
@@ -551,7 +553,8 @@ rag_status packed_linear_i8(const int8_t* x, int32_t ldx, const float* x_scale, 
 
 /*
  * Causal attention with a sliding window and first tokens that stay visible
- * (sinks), bf16 or fp32, fused like ragged_attention: position p sees the keys
+ * (sinks), bf16 or fp32, fused like ragged_attention, with no rounding to bf16 but the
+ * result's: position p sees the keys
  *   j <= p  with  j > p - window  or  j < sinks
  * (window >= 0, sinks >= 0; a window of INT32_MAX is ragged_attention_causal's mask).
  * A position that sees no key (window 0 and no sinks) gets zeros.  Query head h

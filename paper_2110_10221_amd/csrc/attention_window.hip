@@ -28,18 +28,19 @@
 // Nothing is rounded but the result.  In bf16 the P V product takes each exponential as two bf16
 // values, its rounding and the rest (2^-16 of it is lost): the result is 1.65e-3 from the exact one
 // by its norm, its own rounding, where one value gives 2.29e-3 (six prompts of 1500 to 8192 tokens,
-// window 1024, 16/4 heads, 145 us with one, 186 with two; two of 8192, all visible, 16/8 heads, 436 and 581; 32 single
-// tokens 31.1 either way, they wait for memory).  fp32
-// products round nothing; they run on v_mfma_f32_16x16x4f32, 16 keys (4 for P V) by 16 rows at a time, and only
-// those that any row sees: a window of 96 is 111 keys to 16 rows, to 32 x 32 blocks it was 160 (batch 32 of
-// 16 to 512 tokens, 8 heads: 50.9 us on those, 46.5; 64 single tokens, caches to 2048, 8 heads 87, 79; six prompts
-// of 1500 to 8192 tokens, window 1024 933, 948).
-// What bounds it: for prompts the vector work of the softmax, about 420 cycles of a chunk and wave beside
-// 256 of MFMAs that pass under another wave's, and the copies into LDS (six prompts of 1500 to 8192
-// tokens, window 1024, 16/4 heads: 147 us, 700 TFLOP/s; timed without its exponentials 8% less, without its copies
-// 14%, without half of its MFMAs 3%), in fp32 the 4096 MFMA cycles of a chunk; for single tokens the bytes of K and V: 32
-// tokens over 4100 keys of 4 heads each, 134 MB, 28 us (4.8 TB/s; a large copy reaches 5.2) and 4.8 for
-// the join.
+// window 1024, 16/4 heads, 145 us with one, 186 with two; two of 8192, all visible, 16/8 heads, 436 and 581;
+// 32 single tokens 31.1 either way, they wait for memory; the times above are with one).  fp32
+// products run on v_mfma_f32_16x16x4f32, 16 keys (4 for P V) by 16 rows at a time, and only
+// those that any row sees: a window of 96 is 111 keys to 16 rows, to 32 x 32 blocks it was 160 (a tenth of the time of
+// batch 32 of 16 to 512 tokens, 8 heads, and of 64 single tokens, caches to 2048, 8 heads; six prompts
+// of 1500 to 8192 tokens, window 1024, take 2% more).
+// What bounds it: for prompts the vector instructions and the MFMAs, whose cycles add up to the launch (60% and
+// 41% of a SIMD's: 552 and 384 for a chunk and wave, of 927), for they do not pass under one another (six
+// prompts of 1500 to 8192 tokens, window 1024, 16/4 heads: 186 us, 550 TFLOP/s of visible pairs).  In fp32 latency: batch 32 of
+// 16 to 512 tokens, window 96, 8 heads, 40 us, has its matrix units busy for 24% of the time and its vector units for 8%, with 1.1
+// waves on a SIMD (179 registers allow two, and 1200 workgroups are a round of 1024 and the start of another).  For single
+// tokens the bytes of K and V: 32 tokens over 4100 keys of 4 heads each, 134 MB, 28 us (4.8 TB/s; a
+// large copy reaches 5.2) and 4.5 for the join.
 #include <algorithm>
 #include <cfloat>
 #include <type_traits>
@@ -679,9 +680,9 @@ hipError_t launch_attention_window(const PlanView& p, int dtype, const void* q, 
     // Tiles of 128 rows, whose four waves share a chunk's copies, in bf16 from groups of four on (their
     // positions span at most a chunk, else the waves wait for each other's first and last ones), where two entries
     // of a key head always make one (an odd group's would leave workgroups empty).  Us on 64 and 128
-    // rows: six prompts of 1500 to 8192 tokens, 16/4 heads, window 1024 163, 156; 128 sequences to 512
-    // tokens, 16/4 heads, window 128 55.5, 54.1; 256 of 17 tokens 16.1, 12.4; groups of two, 16 of 300
-    // tokens, 8/4 heads 10.3, 11.2; two of 8192, 16/8 heads 430, 442.  fp32, bound by its MFMAs: equal.
+    // rows: six prompts of 1500 to 8192 tokens, 16/4 heads, window 1024 198, 190; 128 sequences to 512
+    // tokens, 16/4 heads, window 128 66.0, 60.0; 256 of 17 tokens 18.2, 14.3; groups of two, 16 of 300
+    // tokens, 8/4 heads 12.4, 12.8; two of 8192, 16/8 heads 593, 641.  fp32: equal.
     const bool wide = dtype == 1 && !single && splits == 1 && group >= 4 && group % 2 == 0;
     const int stride = single ? group : wide ? 2 : 1, dealt = !single && splits == 1;
     const uint32_t magic = group == 1 ? 0u : 0xffffffffu / (uint32_t)group + 1u;
