@@ -571,7 +571,9 @@ rag_status packed_linear_i8(const int8_t* x, int32_t ldx, const float* x_scale, 
  *
  * q and out are [T, H * hd]; q, k, v and out are 16-byte aligned with rows that are
  * multiples of 16 bytes, below 2^22 elements; out overlaps nothing.  H is at most 32768.  Keys and
- * values that a position does not see never reach its output, infinities and NaN among them.  `workspace` (16-byte aligned) holds at least the
+ * values that a position does not see never reach its output, infinities and NaN among them; an infinite
+ * value that it sees makes that channel infinite, however small its weight (NaN with a NaN or an infinity of the
+ * other sign).  `workspace` (16-byte aligned) holds at least the
  * bytes that ragged_attention_window_workspace gives for the same host values, used when few
  * rows over many keys are split; it needs no clearing, and calls that overlap in time
  * need one each.  (max_kv_len is max_len for ragged_attention_window.)

@@ -19,7 +19,7 @@
 //           window begins later would raise theirs from nothing, a recomputation each tile.
 //   masks   only in chunks that cut some row's range; a chunk no row of a wave sees is
 //           skipped by it.  Hidden values are multiplied by a zero, so those that are not
-//           finite are taken out of such a chunk's operand and added to the rows that see
+//           finite are taken out of such a chunk's operand and given to the rows that see
 //           them after the last chunk (in the loop their handling cost 35 registers, the
 //           fourth wave per SIMD: six prompts of 1500 to 8192 tokens 172 us, 161 without, when
 //           it was moved).  The masks are bits of a word per row and chunk (166 us, 161).
@@ -412,7 +412,7 @@ void k_attention_window(WinArgs a) {
 #pragma unroll
         for (int b = 0; b < RB; ++b) lsum[b] += ps[b];
         // Values that are not finite, among hidden keys, would reach every row (0 times infinity): they
-        // are taken out of the operand here and added after the last chunk.
+        // are taken out of the operand here and looked for after the last chunk.
         if constexpr (BF16) {
             if (!whole) {
                 typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
@@ -501,11 +501,29 @@ void k_attention_window(WinArgs a) {
         step(i, std::integral_constant<int, 0>{});
         if (i + 1 < i1) step(i + 1, std::integral_constant<int, kStage>{});
     }
-    if (infinite) {  // (a positive weight leaves an infinity or NaN what it is)
+    // Values that are not finite: a positive weight leaves them what they are, where products with an
+    // exponential's second part, or with one too small for fp32, may be NaN.  Outputs that are not finite are
+    // looked into too (unless the row's weights are not: a NaN stays).
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+        float odd[4] = {0.f, 0.f, 0.f, 0.f};  // NaN with any
+#pragma unroll
+        for (int cb = 0; cb < NO; ++cb)
+#pragma unroll
+            for (int e = 0; e < EO; ++e) odd[e % 4] = fmaf(oacc[b][cb][e], 0.f, odd[e % 4]);
+        const float all = (odd[0] + odd[1]) + (odd[2] + odd[3]);
+        infinite |= all != all && finite_f32(lsum[b]);
+    }
+    if (__builtin_expect(__ballot(infinite) != 0, 0)) {
+        Out found[RB][NO];
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int cb = 0; cb < NO; ++cb)
+#pragma unroll
+                for (int e = 0; e < EO; ++e) found[b][cb][e] = 0.f;
         for (int i = i0; i < i1; ++i) {
-            const int c = chunk(i);
-            if (c >= whole0 && c < whole1) continue;  // its products took them as they are
-            for (int j = c * kWinChunk; j < (c + 1) * kWinChunk; ++j) {
+            for (int j = chunk(i) * kWinChunk, j1 = j + kWinChunk; j < j1; ++j) {
                 const T* const vrow = vbase + (int64_t)j * a.ldv + 4 * part;
 #pragma unroll
                 for (int b = 0; b < RB; ++b) {
@@ -517,11 +535,18 @@ void k_attention_window(WinArgs a) {
                             float x;
                             if constexpr (BF16) x = bf16_to_f32(vrow[WO * cb + 8 * (e / 4) + e % 4]);
                             else x = vrow[WO * cb + e];
-                            if (!finite_f32(x)) oacc[b][cb][e] += x;
+                            if (!finite_f32(x)) found[b][cb][e] += x;
                         }
                 }
             }
         }
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int cb = 0; cb < NO; ++cb)
+#pragma unroll
+                for (int e = 0; e < EO; ++e)
+                    if (found[b][cb][e] != 0.f && finite_f32(lsum[b])) oacc[b][cb][e] = found[b][cb][e];
     }
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
@@ -602,7 +627,10 @@ __global__ __launch_bounds__(256) void k_attention_window_join(WinArgs a) {
         const float w = i < n ? __builtin_amdgcn_exp2f(ms[i] - m) : 0.f;
         sum = fmaf(w, ls[i], sum);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = fmaf(w, os[i][e], o[e]);
+        for (int e = 0; e < 4; ++e) {
+            const float x = i < n ? os[i][e] : 0.f;
+            o[e] = finite_f32(x) ? fmaf(w, x, o[e]) : o[e] + x;  // (a weight may be too small for fp32, not zero)
+        }
     }
     if constexpr (GROUPS > 1) {  // the wave's four groups, then the four waves
 #pragma unroll

@@ -491,3 +491,50 @@ def test_a_scale_of_zero_keeps_what_is_not_finite(dtype, bad):
     rag.ragged_attention_window(plan, q.cuda(), k.cuda(), v.cuda(), out, 0.0, 10, 1)
     nan = torch.isnan(out.cpu().float())
     assert nan[20, 64:].all() and nan.sum() == 64
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.125, 3.0])
+@pytest.mark.parametrize("L,kv_len,window,sinks", [([300, 70], None, ALL, 0), ([300, 70], None, 150, 3), ([1, 3], [5000, 700], ALL, 0)])
+def test_values_that_are_not_finite_reach_the_rows_that_see_them(dtype, scale, L, kv_len, window, sinks):
+    # as they are, whatever the weight (those of scale 3 are too small for fp32 for many keys), in chunks that a row sees
+    # whole, in cut ones and over split keys: infinity, minus infinity, NaN, and NaN where both infinities meet
+    import paper_2110_10221_amd as rag
+
+    H, KV, n = 8, 2, kv_len or L
+    first, T, rows = np.concatenate([[0], np.cumsum(n)[:-1]]).tolist(), sum(L), sum(n)
+    q, k, v = (P.normal(s, r, w, dtype=dtype, std=d) for s, r, w, d in ((1, T, H * 64, 2.0), (2, rows, KV * 64, 1.0), (3, rows, KV * 64, 1.0)))
+    inf, nan = float("inf"), float("nan")
+    bad = torch.zeros(rows, KV * 64, dtype=torch.float64)
+    for b in range(len(n)):
+        for channel, at in ((3, {20: inf}), (9, {40: -inf}), (17, {33: nan}), (30, {5: inf, 45: -inf}), (64 + 41, {n[b] - 1: inf}),
+                            (64 + 50, {n[b] // 2: -inf, n[b] // 2 + 1: -inf})):
+            for j, x in at.items():
+                bad[first[b] + j, channel] = x
+    dirty = torch.where(bad != 0, bad, v.double()).to(v.dtype)
+    plan, out = make_plan(L, H), torch.empty(T, H * 64, dtype=q.dtype, device="cuda")
+    ws = torch.empty(rag.ragged_attention_window_workspace(plan, max(n), window, sinks, KV, q.dtype), dtype=torch.uint8, device="cuda")
+    if kv_len:
+        assert ws.numel() > 0
+        rag.ragged_attention_window_cached(plan, q.cuda(), k.cuda(), dirty.cuda(), torch.tensor(first).cuda(),
+                                           torch.tensor(n, dtype=torch.int32).cuda(), max(n), out, scale, window, sinks, KV, workspace=ws)
+    else:
+        rag.ragged_attention_window(plan, q.cuda(), k.cuda(), dirty.cuda(), out, scale, window, sinks, KV, workspace=ws)
+    clean = torch.where(bad != 0, 0.0, v.double()).to(v.dtype)
+    ref, mag, bound, count = P.window_attention(L, H, KV, q, k, clean, first, n, window, sinks, scale)
+    tol = P.window_tolerance(dtype, ref, mag, bound, count)
+    got, t0 = out.cpu().double(), 0
+    for b in range(len(n)):
+        p, j = torch.arange(n[b] - L[b], n[b])[:, None], torch.arange(n[b])[None]
+        seen = (j <= p) & ((j > p - window) | (j < sinks))
+        x = bad[first[b]:first[b] + n[b]]
+        some = lambda m: (seen.double() @ m.double()) > 0  # noqa: E731
+        up, down, none = some(x == inf), some(x == -inf), some(torch.isnan(x))
+        none = none | (up & down)
+        want = torch.where(none, nan, torch.where(up, inf, torch.where(down, -inf, 0.0)))
+        want = want.reshape(-1, KV, 1, 64).expand(-1, KV, H // KV, 64).reshape(L[b], H * 64)
+        at = slice(t0, t0 + L[b])
+        special = want != 0
+        assert torch.equal(torch.nan_to_num(got[at][special], 7.0, 8.0, 9.0), torch.nan_to_num(want[special], 7.0, 8.0, 9.0))
+        assert ((got[at] - ref[at]).abs() <= tol[at])[~special].all()
+        t0 += L[b]
