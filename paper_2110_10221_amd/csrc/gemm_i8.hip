@@ -113,13 +113,17 @@ struct Finish {
     }
     __device__ __forceinline__ void row(const I8Args& a, const int* sum, float xs, bool residual, const Raw& res, int m, int n) const {
         float v[8];
-        // (one branch for the wave: two ways for each lane cost 35475 x 1024 x 1024 59.0 -> 61.8 us, this nothing)
-        if (__builtin_expect(__ballot(!(fabsf(xs) <= 0x1p96f)) == 0, 1)) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = fmaf((float)sum[e] * xs, ws[e >> 2][e & 3], bv[e]);
-        } else {  // the sums, up to 2^31, may pass fp32's range before the features' scales bring them back
+        for (int e = 0; e < 8; ++e) v[e] = fmaf((float)sum[e] * xs, ws[e >> 2][e & 3], bv[e]);
+        // The sums, up to 2^31, may pass fp32's range before the features' scales bring them back.  (One branch for
+        // the wave: two ways for each lane cost 35475 x 1024 x 1024 59.0 -> 61.8 us, this nothing.)
+        const bool far = fabsf(xs) > 0x1p96f;
+        if (__builtin_expect(__ballot(far) != 0, 0)) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = (float)fma((double)sum[e] * xs, (double)ws[e >> 2][e & 3], (double)bv[e]);
+            for (int e = 0; e < 8; ++e) {
+                const float z = (float)fma((double)sum[e] * xs, (double)ws[e >> 2][e & 3], (double)bv[e]);
+                v[e] = far ? z : v[e];
+            }
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = finish_act<BF16, ACT>(v[e]);

@@ -219,3 +219,20 @@ def test_scales_near_the_range(T, dtype):
     ref = lin + b.double()
     tol = F32 * (4 * lin.abs() + b.double().abs() + 2 * ref.abs()) + P.HALF[dtype] * ref.abs()
     assert ((y.cpu().double() - ref).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("odd", [float("nan"), float("inf"), 2e36])
+@pytest.mark.parametrize("T", [4, 70])
+def test_a_token_does_not_depend_on_its_neighbours_scales(T, odd):
+    import paper_2110_10221_amd as rag
+
+    x, w = int8(1, T, 272).cuda(), int8(2, 264, 272).cuda()
+    xs, ws = scales(3, T).cuda(), scales(4, 264).cuda()
+    outs = []
+    for scale in (1.0, odd):
+        xs[1] = scale
+        y = torch.empty(T, 264, device="cuda")
+        rag.packed_linear_i8(x, xs, w, ws, y, P.normal(5, 264, dtype="f32").cuda())
+        outs.append(y.cpu())
+    rest = torch.arange(T) != 1
+    assert torch.equal(outs[0][rest], outs[1][rest])
