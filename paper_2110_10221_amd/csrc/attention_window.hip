@@ -37,7 +37,7 @@
 // What bounds it: for prompts the vector instructions and the MFMAs, whose cycles add up to the launch (60% and
 // 41% of a SIMD's: 552 and 384 for a chunk and wave, of 927), for they do not pass under one another (six
 // prompts of 1500 to 8192 tokens, window 1024, 16/4 heads: 186 us, 550 TFLOP/s of visible pairs).  In fp32 latency: batch 32 of
-// 16 to 512 tokens, window 96, 8 heads, 40 us, has its matrix units busy for 24% of the time and its vector units for 8%, with 1.1
+// 16 to 512 tokens, window 96, 8 heads, 40 us, has its matrix units busy for 24% of the time and its vector units for 9%, with 1.1
 // waves on a SIMD (179 registers allow two, and 1200 workgroups are a round of 1024 and the start of another).  For single
 // tokens the bytes of K and V: 32 tokens over 4100 keys of 4 heads each, 134 MB, 28 us (4.8 TB/s; a
 // large copy reaches 5.2) and 4.5 for the join.
